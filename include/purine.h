@@ -57,7 +57,11 @@
 extern "C" {
 #endif
 
-typedef enum { PURINE_F32 = 0, PURINE_BF16 = 1, PURINE_I32 = 2 } purine_dtype;
+typedef enum {
+    PURINE_F32 = 0, PURINE_BF16 = 1, PURINE_I32 = 2,
+    PURINE_F8 = 3            /* OCP e4m3 bit patterns: the 8-bit states of purine_adamw_step
+                                (purine_block.h), nothing else */
+} purine_dtype;
 
 typedef enum {
     PURINE_OK = 0,

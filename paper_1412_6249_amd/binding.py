@@ -2,7 +2,7 @@
 module _marshal (a ctypes descriptor costs 1.6 us each, more than a launch); everything else, and whatever _marshal
 hands back as not the plain case (None), through ctypes.
 
-Every function has the name of the C entry point it calls (see include/purine.h). Tensors are
+Every function has the name of the C entry point it calls (see include/purine.h and include/purine_block.h). Tensors are
 torch tensors that live on the GPU (PyTorch supplies device memory and streams, nothing else);
 each call raises PurineError on a non-zero status. There is no fallback path: if the shared
 library or _marshal.so is missing, importing this module fails.
@@ -17,7 +17,7 @@ import torch  # noqa: F401
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libpurine_conv.so")
 
-PURINE_F32, PURINE_BF16, PURINE_I32 = 0, 1, 2
+PURINE_F32, PURINE_BF16, PURINE_I32, PURINE_F8 = 0, 1, 2, 3
 PURINE_CONV_FWD, PURINE_CONV_BWD_DATA, PURINE_CONV_BWD_WEIGHT, PURINE_CONV_BWD_WEIGHT_BIAS = 0, 1, 2, 3
 
 OP_CONV_FWD, OP_BIAS_FWD, OP_CONV_BWD_DATA, OP_CONV_BWD_WEIGHT, OP_BIAS_BWD = 0, 1, 2, 3, 4
@@ -27,6 +27,11 @@ OP_CONV_FWD_BIAS_RELU, OP_CONV_BWD_DATA_RELU, OP_CONV_BWD_WEIGHT_BIAS, OP_SGD_UP
 OP_FC_FWD, OP_FC_BWD_DATA, OP_FC_BWD_WEIGHT = 18, 19, 20
 OP_GROUPED_CONV_FWD, OP_GROUPED_CONV_BWD_DATA, OP_GROUPED_CONV_BWD_WEIGHT = 21, 22, 23
 OP_MAXPOOL_BWD_RELU = 24
+
+PURINE_ACT_NONE, PURINE_ACT_RELU, PURINE_ACT_SILU, PURINE_ACT_GELU, PURINE_ACT_GELU_TANH = 0, 1, 2, 3, 4
+ACTIVATIONS = {"none": PURINE_ACT_NONE, "relu": PURINE_ACT_RELU, "silu": PURINE_ACT_SILU, "gelu": PURINE_ACT_GELU,
+               "gelu_tanh": PURINE_ACT_GELU_TANH}
+PURINE_ADAMW_BLOCK = 256
 
 STATUS = {0: "PURINE_OK", -1: "PURINE_E_NULL", -2: "PURINE_E_SHAPE", -3: "PURINE_E_DTYPE",
           -4: "PURINE_E_LAYOUT", -5: "PURINE_E_WORKSPACE", -6: "PURINE_E_GRAPH",
@@ -60,6 +65,15 @@ class purine_op_attrs(ctypes.Structure):
     _fields_ = [("conv", purine_conv_desc), ("pool", purine_pool_desc), ("beta", ctypes.c_float),
                 ("relu", ctypes.c_int32), ("ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t),
                 ("lr", ctypes.c_float), ("groups", ctypes.c_int32)]
+
+
+class purine_adamw_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + [
+        ("step", ctypes.c_int32), ("seed", ctypes.c_uint32), ("dither", ctypes.c_int32)]
+
+
+class purine_adamw_param(ctypes.Structure):
+    _fields_ = [(n, purine_tensor) for n in ("w", "dw", "m", "v", "m_scale", "v_scale", "copy")]
 
 
 if not os.path.exists(LIB_PATH):
@@ -135,11 +149,25 @@ _SIGS = {
     "purine_graph_op_elapsed_ms": (ctypes.c_int, [_vp, ctypes.c_int, _P(ctypes.c_float)]),
     "purine_set_kernel_probe": (None, [_vp, _vp]),
 }
-for _name, (_res, _args) in _SIGS.items():
+# include/purine_block.h
+_BLOCK_SIGS = {
+    "purine_group_norm_workspace_bytes": (_sz, [ctypes.c_int, _i64p, ctypes.c_int, ctypes.c_int, ctypes.c_int32]),
+    "purine_group_norm_fwd": (ctypes.c_int, [_T] * 6 + [ctypes.c_int, ctypes.c_float, ctypes.c_int, _vp, _sz, _vp]),
+    "purine_group_norm_bwd": (ctypes.c_int, [_T] * 9 + [ctypes.c_int, ctypes.c_int, ctypes.c_float, _vp, _sz, _vp]),
+    "purine_linear_workspace_bytes": (_sz, [ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32]),
+    "purine_linear_fwd": (ctypes.c_int, [_T] * 6 + [ctypes.c_int, _vp, _sz, _vp]),
+    "purine_linear_bwd_data": (ctypes.c_int, [_T] * 4 + [ctypes.c_int, ctypes.c_float, _vp, _sz, _vp]),
+    "purine_linear_bwd_weight": (ctypes.c_int, [_T] * 4 + [ctypes.c_float, _vp, _sz, _vp]),
+    "purine_act_bwd_workspace_bytes": (_sz, [ctypes.c_int64, ctypes.c_int64]),
+    "purine_act_bwd": (ctypes.c_int, [_T] * 4 + [ctypes.c_int, _vp, _sz, _vp]),
+    "purine_adamw_step": (ctypes.c_int, [_P(purine_adamw_desc), _P(purine_adamw_param), ctypes.c_int, _T, _vp]),
+}
+for _name, (_res, _args) in [*_SIGS.items(), *_BLOCK_SIGS.items()]:
     _f = getattr(_lib, _name)
     _f.restype, _f.argtypes = _res, _args
 
 EXPORTED = sorted(_SIGS)
+EXPORTED_BLOCK = sorted(_BLOCK_SIGS)
 # include/purine_introspect.h
 _lib.purine_conv_matrix_products.restype = ctypes.c_int
 _lib.purine_conv_matrix_products.argtypes = [ctypes.c_int, _D, _i64p, _i64p, ctypes.c_int32]
@@ -183,6 +211,16 @@ def tensor_desc(t):
     d.ndim = t.dim()
     for i, v in enumerate(t.shape):
         d.dim[i] = int(v)
+    return d
+
+
+def matrix_desc(t):
+    """purine_tensor of a matrix whose rows may lie apart (columns of a wider one); anything else as tensor_desc."""
+    if isinstance(t, purine_tensor) or t.dim() != 2 or t.is_contiguous() or t.stride(1) != 1 or t.stride(0) < t.shape[1]:
+        return tensor_desc(t)
+    d = tensor_desc(t.as_strided((1, 1), (1, 1)))
+    d.dim[0], d.dim[1] = int(t.shape[0]), int(t.shape[1])
+    d.nstride = int(t.stride(0))
     return d
 
 
@@ -424,6 +462,124 @@ def purine_sgd_update(w, dw, new_w, lr, stream=None):
         rc = _lib.purine_sgd_update(_ref(tensor_desc(w)), _ref(tensor_desc(dw)), _ref(tensor_desc(new_w)),
             float(lr), _stream(stream))
     _check(rc, "purine_sgd_update")
+
+
+def purine_group_norm_workspace_bytes(backward, x_shape, groups, dtype=PURINE_F32):
+    """x_shape: 2 to 4 extents, images first, channels last."""
+    dims = [int(v) for v in x_shape]
+    return int(_lib.purine_group_norm_workspace_bytes(1 if backward else 0, (ctypes.c_int64 * 4)(*dims[:4]), len(dims), int(groups), int(dtype)))
+
+
+def purine_group_norm_fwd(x, scale, shift, y, mean, rstd, groups, eps=1e-5, act=PURINE_ACT_NONE, ws=None, stream=None):
+    rc = _marshal.purine_group_norm_fwd(x, scale, shift, y, mean, rstd, groups, eps, act, ws, stream)
+    if rc is None:
+        p, n = _ws(ws)
+        rc = _lib.purine_group_norm_fwd(_ref(tensor_desc(x)), _opt(scale), _opt(shift), _ref(tensor_desc(y)), _opt(mean), _opt(rstd),
+            int(groups), float(eps), int(act), p, n, _stream(stream))
+    _check(rc, "purine_group_norm_fwd")
+
+
+def purine_group_norm_bwd(x, scale, shift, mean, rstd, dy, dx, dscale, dshift, groups, act=PURINE_ACT_NONE, beta=0.0, ws=None,
+                          stream=None):
+    rc = _marshal.purine_group_norm_bwd(x, scale, shift, mean, rstd, dy, dx, dscale, dshift, groups, act, beta, ws, stream)
+    if rc is None:
+        p, n = _ws(ws)
+        rc = _lib.purine_group_norm_bwd(_ref(tensor_desc(x)), _opt(scale), _opt(shift), _ref(tensor_desc(mean)), _ref(tensor_desc(rstd)),
+            _ref(tensor_desc(dy)), _ref(tensor_desc(dx)), _opt(dscale), _opt(dshift), int(groups), int(act), float(beta), p, n,
+            _stream(stream))
+    _check(rc, "purine_group_norm_bwd")
+
+
+def _opt_matrix(t):
+    return _ref(matrix_desc(t)) if t is not None else None
+
+
+def purine_linear_workspace_bytes(which, N, C, K, dtype=PURINE_F32):
+    return int(_lib.purine_linear_workspace_bytes(int(which), int(N), int(C), int(K), int(dtype)))
+
+
+def purine_linear_fwd(x, w, b, r, y, pre=None, act=PURINE_ACT_NONE, ws=None, stream=None):
+    rc = _marshal.purine_linear_fwd(x, w, b, r, y, pre, act, ws, stream)
+    if rc is None:
+        p, n = _ws(ws)
+        rc = _lib.purine_linear_fwd(_ref(matrix_desc(x)), _ref(matrix_desc(w)), _opt(b), _opt_matrix(r), _ref(matrix_desc(y)),
+            _opt_matrix(pre), int(act), p, n, _stream(stream))
+    _check(rc, "purine_linear_fwd")
+
+
+def purine_linear_bwd_data(dy, w, pre, dx, act=PURINE_ACT_NONE, beta=0.0, ws=None, stream=None):
+    rc = _marshal.purine_linear_bwd_data(dy, w, pre, dx, act, beta, ws, stream)
+    if rc is None:
+        p, n = _ws(ws)
+        rc = _lib.purine_linear_bwd_data(_ref(matrix_desc(dy)), _ref(matrix_desc(w)), _opt_matrix(pre), _ref(matrix_desc(dx)), int(act),
+            float(beta), p, n, _stream(stream))
+    _check(rc, "purine_linear_bwd_data")
+
+
+def purine_linear_bwd_weight(x, dy, dw, db=None, beta=0.0, ws=None, stream=None):
+    rc = _marshal.purine_linear_bwd_weight(x, dy, dw, db, beta, ws, stream)
+    if rc is None:
+        p, n = _ws(ws)
+        rc = _lib.purine_linear_bwd_weight(_ref(matrix_desc(x)), _ref(matrix_desc(dy)), _ref(matrix_desc(dw)), _opt(db), float(beta), p, n,
+            _stream(stream))
+    _check(rc, "purine_linear_bwd_weight")
+
+
+def purine_act_bwd_workspace_bytes(N, K):
+    return int(_lib.purine_act_bwd_workspace_bytes(int(N), int(K)))
+
+
+def purine_act_bwd(pre, dy, g, db=None, act=PURINE_ACT_NONE, ws=None, stream=None):
+    rc = _marshal.purine_act_bwd(pre, dy, g, db, act, ws, stream)
+    if rc is None:
+        p, n = _ws(ws)
+        rc = _lib.purine_act_bwd(_ref(matrix_desc(pre)), _ref(matrix_desc(dy)), _ref(matrix_desc(g)), _opt(db), int(act), p, n,
+            _stream(stream))
+    _check(rc, "purine_act_bwd")
+
+
+def adamw_desc(lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=1.0, step=1, seed=0, dither=False):
+    return purine_adamw_desc(lr, beta1, beta2, eps, weight_decay, grad_scale, int(step), int(seed) & 0xffffffff, 1 if dither else 0)
+
+
+class AdamwParams:
+    """The tensors of purine_adamw_step as descriptors, made once and kept (with the tensors) from step to step."""
+
+    def __init__(self, array, tensors):
+        self.array, self.tensors = array, tensors
+
+    def __len__(self):
+        return len(self.array)
+
+
+def _adamw_tensor_desc(t):
+    if getattr(t, "dtype", None) != torch.float8_e4m3fn:
+        return tensor_desc(t)
+    if not t.is_cuda:
+        raise ValueError("tensor must live on the GPU")
+    if t.dim() < 1 or t.dim() > 4 or not t.is_contiguous():
+        raise ValueError("1 to 4 dimensions, contiguous")
+    return raw_desc(t.data_ptr(), PURINE_F8, t.shape)
+
+
+def adamw_params(w, dw, m, v, m_scale=None, v_scale=None, copy=None):
+    """Lists of as many tensors each (m_scale, v_scale: with 8-bit states; copy: may be None or hold None)."""
+    n = len(w)
+    lists = {"w": w, "dw": dw, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "copy": copy}
+    for name, l in lists.items():
+        if l is not None and len(l) != n:
+            raise ValueError("%s: %d tensors, and %d of w" % (name, len(l), n))
+    array = (purine_adamw_param * n)()
+    for name, l in lists.items():
+        for i, t in enumerate(l or ()):
+            if t is not None:
+                setattr(array[i], name, _adamw_tensor_desc(t))
+    return AdamwParams(array, lists)
+
+
+def purine_adamw_step(desc, params, done=None, stream=None):
+    """params: what adamw_params returned. done: int32 tensor of one element with the steps done before, or None."""
+    _check(_lib.purine_adamw_step(_ref(desc), params.array, len(params), _opt(done), _stream(stream)), "purine_adamw_step")
 
 
 def purine_bias_fwd(b, y, stream=None):

@@ -18,16 +18,17 @@
 #include <tuple>
 #include <type_traits>
 
-#include "purine.h"
+#include "purine_block.h"
 
 namespace {
 
-constexpr int MAX_TENSORS = 5;
+constexpr int MAX_TENSORS = 9;
 
 struct Call {
     PyObject* const* args;
     Py_ssize_t n, next = 0;
     unsigned optional;                       // tensor arguments that may be None
+    bool rows;                               // matrices may have rows apart
     purine_tensor t[MAX_TENSORS];
     int tensors = 0;
     void* ws = nullptr;
@@ -46,7 +47,7 @@ PyTypeObject* descriptor_type[2] = {nullptr, nullptr};     // purine_conv_desc, 
 
 bool is_descriptor(PyObject* o, int which) { return descriptor_type[which] && PyObject_TypeCheck(o, descriptor_type[which]); }
 
-bool fill(purine_tensor& d, PyObject* o) {
+bool fill(purine_tensor& d, PyObject* o, bool rows) {
     if (!THPVariable_Check(o)) return false;
     const at::Tensor& t = THPVariable_Unpack(o);
     if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided) return false;
@@ -60,7 +61,10 @@ bool fill(purine_tensor& d, PyObject* o) {
     }
     d.nstride = 0;
     for (int i = 0; i < 4; ++i) d.dim[i] = i < dims ? t.size(i) : 0;
-    if (!t.is_contiguous()) {                // a channel slice of a contiguous NCHW tensor
+    if (!t.is_contiguous() && rows && dims == 2) {
+        if (t.stride(1) != 1 || t.stride(0) < d.dim[1]) return false;
+        d.nstride = t.stride(0);
+    } else if (!t.is_contiguous()) {         // a channel slice of a contiguous NCHW tensor
         if (dims != 4 || t.stride(3) != 1 || t.stride(2) != d.dim[3] || t.stride(1) != d.dim[2] * d.dim[3] ||
             t.stride(0) < d.dim[1] * d.dim[2] * d.dim[3]) return false;
         d.nstride = t.stride(0);
@@ -77,7 +81,7 @@ A take(Call& c) {
         const int i = c.tensors++;
         if (!c.ok || i >= MAX_TENSORS) { c.ok = false; return nullptr; }
         if (o == Py_None && (c.optional >> i & 1)) return nullptr;
-        if (!fill(c.t[i], o)) c.ok = false;
+        if (!fill(c.t[i], o, c.rows)) c.ok = false;
         return &c.t[i];
     } else if constexpr (std::is_same_v<A, const purine_conv_desc*> || std::is_same_v<A, const purine_pool_desc*>) {
         PyObject* o = c.arg();
@@ -121,11 +125,12 @@ A take(Call& c) {
 }
 
 template <typename... A>
-PyObject* invoke(int (*fn)(A...), PyObject* const* args, Py_ssize_t n, unsigned optional) {
+PyObject* invoke(int (*fn)(A...), PyObject* const* args, Py_ssize_t n, unsigned optional, bool rows) {
     constexpr int POINTERS = (0 + ... + (std::is_same_v<A, void*> ? 1 : 0));
     try {
         Call c{args, n};
         c.optional = optional;
+        c.rows = rows;
         std::tuple<A...> a{take<A, POINTERS>(c)...};                    // (braces: in order)
         if (!c.ok || c.next != n) Py_RETURN_NONE;
         // (noexcept: an exception out of a C entry ends the program, as from ctypes; it must not be taken for "not the plain case")
@@ -141,16 +146,22 @@ PyObject* invoke(int (*fn)(A...), PyObject* const* args, Py_ssize_t n, unsigned 
     }
 }
 
-#define ENTRY(NAME, OPTIONAL)                                                                    \
-    PyObject* call_##NAME(PyObject*, PyObject* const* args, Py_ssize_t n) { return invoke(&NAME, args, n, OPTIONAL); }
+#define ENTRY_(NAME, OPTIONAL, ROWS)                                                             \
+    PyObject* call_##NAME(PyObject*, PyObject* const* args, Py_ssize_t n) { return invoke(&NAME, args, n, OPTIONAL, ROWS); }
+#define ENTRY(NAME, OPTIONAL) ENTRY_(NAME, OPTIONAL, false)
+#define MATRIX_ENTRY(NAME, OPTIONAL) ENTRY_(NAME, OPTIONAL, true)
+#define MATRIX_ENTRIES(X)                                                                        \
+    X(purine_linear_fwd, 44) X(purine_linear_bwd_data, 4) X(purine_linear_bwd_weight, 8) X(purine_act_bwd, 8)
 #define ENTRIES(X)                                                                               \
     X(purine_conv_fwd, 0) X(purine_conv_fwd_bias_relu, 4) X(purine_conv_bwd_data, 0) X(purine_conv_bwd_data_relu, 0)        \
     X(purine_conv_bwd_weight, 0) X(purine_conv_bwd_weight_bias, 0) X(purine_conv_bwd_weight_static, 0)                     \
     X(purine_grouped_conv_fwd, 4) X(purine_grouped_conv_bwd_data, 0) X(purine_grouped_conv_bwd_weight, 8)                  \
     X(purine_fc_fwd, 4) X(purine_fc_bwd_data, 0) X(purine_fc_bwd_weight, 8) X(purine_sgd_update, 0)                        \
     X(purine_bias_fwd, 0) X(purine_bias_bwd, 0) X(purine_relu_fwd, 0) X(purine_relu_bwd, 0)                                \
-    X(purine_maxpool_fwd, 0) X(purine_maxpool_bwd, 0) X(purine_maxpool_bwd_relu, 0)
+    X(purine_maxpool_fwd, 0) X(purine_maxpool_bwd, 0) X(purine_maxpool_bwd_relu, 0)                                       \
+    X(purine_group_norm_fwd, 54) X(purine_group_norm_bwd, 390)
 ENTRIES(ENTRY)
+MATRIX_ENTRIES(MATRIX_ENTRY)
 
 PyObject* descriptor_types(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != 2 || !PyType_Check(args[0]) || !PyType_Check(args[1])) {
@@ -176,7 +187,7 @@ PyObject* takes_descriptor(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 #define METHOD(NAME, OPTIONAL) {#NAME, (PyCFunction)(void (*)(void))&call_##NAME, METH_FASTCALL, nullptr},
-PyMethodDef methods[] = {ENTRIES(METHOD)
+PyMethodDef methods[] = {ENTRIES(METHOD) MATRIX_ENTRIES(METHOD)
     {"descriptor_types", (PyCFunction)(void (*)(void))&descriptor_types, METH_FASTCALL, nullptr},
     {"takes_descriptor", (PyCFunction)(void (*)(void))&takes_descriptor, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
