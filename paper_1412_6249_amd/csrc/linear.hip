@@ -1,8 +1,7 @@
 // Matrix product with bias, activation and residual in its epilogue, its gradients (purine_linear_*), and the gradient of an
 // activation by itself (purine_act_bwd).
-#include "activation.h"
-#include "bf16.h"
-#include "block.h"
+#include "linear_gemm.h"
+#include "packets.h"
 
 namespace purine {
 namespace {
@@ -13,48 +12,44 @@ template <> __device__ __forceinline__ float widen<uint16_t>(uint16_t v) { retur
 __device__ __forceinline__ void narrow(float v, float* p) { *p = v; }
 __device__ __forceinline__ void narrow(float v, uint16_t* p) { *p = f2bf(v); }
 
-struct LinearParams {
-    const void* a; const void* b; void* out;
-    const void* bias; const void* res; void* pre; const void* slope;
-    int64_t a_i, a_k, b_i, b_k, out_ld, res_ld, pre_ld, slope_ld;
-    int rows, cols, K, tiles_j;
+// Element (i, k) of an operand at i * i_step + k * k_step.
+struct Source { const void* p; int64_t i_step, k_step; };
+
+// What the sum goes through on its way to memory (E: the operands' type).
+struct Finish {
+    const void* bias; const void* res; void* pre; const void* slope; void* out;
+    int64_t res_ld, pre_ld, slope_ld, out_ld;
     int act, accumulate;
 };
-
-__device__ __forceinline__ float act_any(int act, float z) {
-    switch (act) {
-        case PURINE_ACT_RELU: return act_of<PURINE_ACT_RELU>(z);
-        case PURINE_ACT_SILU: return act_of<PURINE_ACT_SILU>(z);
-        case PURINE_ACT_GELU: return act_of<PURINE_ACT_GELU>(z);
-        case PURINE_ACT_GELU_TANH: return act_of<PURINE_ACT_GELU_TANH>(z);
-        default: return z;
-    }
-}
-__device__ __forceinline__ float slope_any(int act, float z) {
-    switch (act) {
-        case PURINE_ACT_RELU: return act_slope<PURINE_ACT_RELU>(z);
-        case PURINE_ACT_SILU: return act_slope<PURINE_ACT_SILU>(z);
-        case PURINE_ACT_GELU: return act_slope<PURINE_ACT_GELU>(z);
-        case PURINE_ACT_GELU_TANH: return act_slope<PURINE_ACT_GELU_TANH>(z);
-        default: return 1.0f;
-    }
+template <typename E, typename O>
+__device__ __forceinline__ void finish(const Finish& f, int64_t i, int j, float z) {
+    if (f.bias) z += widen<E>(((const E*)f.bias)[j]);
+    if (f.pre) narrow(z, (E*)f.pre + i * f.pre_ld + j);
+    if (f.slope) z *= slope_any(f.act, widen<E>(((const E*)f.slope)[i * f.slope_ld + j]));
+    else z = act_any(f.act, z);
+    if (f.res) z += widen<E>(((const E*)f.res)[i * f.res_ld + j]);
+    O* o = (O*)f.out + i * f.out_ld + j;
+    if (f.accumulate) z += widen<O>(*o);
+    narrow(z, o);
 }
 
-// The plain kernel: 64 x 64 results per workgroup, 16 per thread, fp32 products.
+// Operands whose rows lie 2^24 elements apart or more, past the 32-bit offsets of the kernels on the matrix cores: 64 x 64 results per
+// workgroup, 16 per thread, fp32 products.
+struct FarParams { Source a, b; Finish f; int rows, cols, K, tiles_j; };
 constexpr int TS = 64, KS = 16;
 template <typename T, typename O>
-__global__ __launch_bounds__(256) void linear_kernel(const LinearParams p) {
+__global__ __launch_bounds__(256) void linear_far_kernel(const FarParams p) {
     __shared__ float as[KS][TS + 1], bs[KS][TS + 1];
     const int i0 = (int)(blockIdx.x / p.tiles_j) * TS, j0 = (int)(blockIdx.x % p.tiles_j) * TS;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const T* a = (const T*)p.a;
-    const T* b = (const T*)p.b;
+    const T* a = (const T*)p.a.p;
+    const T* b = (const T*)p.b.p;
     float acc[4][4] = {};
     for (int k0 = 0; k0 < p.K; k0 += KS) {
         for (int e = threadIdx.x; e < KS * TS; e += 256) {
             const int k = e / TS, i = e % TS;
-            as[k][i] = k0 + k < p.K && i0 + i < p.rows ? widen<T>(a[(i0 + i) * p.a_i + (k0 + k) * p.a_k]) : 0.0f;
-            bs[k][i] = k0 + k < p.K && j0 + i < p.cols ? widen<T>(b[(j0 + i) * p.b_i + (k0 + k) * p.b_k]) : 0.0f;
+            as[k][i] = k0 + k < p.K && i0 + i < p.rows ? widen<T>(a[(i0 + i) * p.a.i_step + (k0 + k) * p.a.k_step]) : 0.0f;
+            bs[k][i] = k0 + k < p.K && j0 + i < p.cols ? widen<T>(b[(j0 + i) * p.b.i_step + (k0 + k) * p.b.k_step]) : 0.0f;
         }
         __syncthreads();
         for (int k = 0; k < KS; ++k)
@@ -64,20 +59,128 @@ __global__ __launch_bounds__(256) void linear_kernel(const LinearParams p) {
     }
     for (int u = 0; u < 4; ++u)
         for (int v = 0; v < 4; ++v) {
-            const int64_t i = i0 + ty * 4 + u;
-            const int j = j0 + tx * 4 + v;
-            if (i >= p.rows || j >= p.cols) continue;
-            float z = acc[u][v];
-            if (p.bias) z += widen<T>(((const T*)p.bias)[j]);
-            if (p.pre) narrow(z, (T*)p.pre + i * p.pre_ld + j);
-            if (p.slope) z *= slope_any(p.act, widen<T>(((const T*)p.slope)[i * p.slope_ld + j]));
-            else z = act_any(p.act, z);
-            if (p.res) z += widen<T>(((const T*)p.res)[i * p.res_ld + j]);
-            O* o = (O*)p.out + i * p.out_ld + j;
-            if (p.accumulate) z += widen<O>(*o);
-            narrow(z, o);
+            const int i = i0 + ty * 4 + u, j = j0 + tx * 4 + v;
+            if (i < p.rows && j < p.cols) finish<T, O>(p.f, i, j, acc[u][v]);
         }
 }
+
+// Lays an operand out in rows of whole 16-byte packets, zeros behind a row's end: bf16 rows that are not, and fp32 ones in three exact bf16
+// parts, a plane each. A thread per packet.
+template <typename T>
+__global__ __launch_bounds__(256) void linear_pack_kernel(const T* __restrict__ src, int64_t ld, uint16_t* __restrict__ dst, int rows, int len, int packets,
+                                                          int64_t plane) {
+    const int64_t total = (int64_t)rows * packets;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
+        const int row = (int)(t / packets), at = (int)(t - (int64_t)row * packets) * 8, n = len - at;
+        const T* s = src + row * ld + at;
+        uint16_t* d = dst + t * 8;
+        if constexpr (sizeof(T) == 2) {
+            uint32_t k[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[e] = (uint32_t)(2 * e < n ? s[2 * e] : 0) | (uint32_t)(2 * e + 1 < n ? s[2 * e + 1] : 0) << 16;
+            *reinterpret_cast<uint4*>(d) = make_uint4(k[0], k[1], k[2], k[3]);
+        } else {
+            float v[8];
+            lin::get8(s, n >= 8 && ld % 4 == 0, n, v);
+            packets::store_split8(v, (unsigned char*)d, (size_t)plane);
+        }
+    }
+}
+
+// Adds the partial sums of the splits in order and finishes the results. A thread has V neighbouring columns of a row, and `lanes`
+// threads share the splits of one (few results of many splits: dw of a narrow layer over many positions). SPLIT3: sums of an fp32 product's parts, to be
+// scaled back; where one is infinite or NaN it is computed again as a plain fp32 sum.
+struct JoinParams { const float* part; Finish f; Source a, b; int rows, cols, K, splits, lanes; };
+template <typename E, typename O, int V>
+__global__ __launch_bounds__(256) void linear_join_kernel(const JoinParams p) {
+    constexpr bool SPLIT3 = sizeof(E) == 4;
+    __shared__ float sums[256][V + 1];
+    const int lanes = p.lanes, per = 256 / lanes, lane = threadIdx.x / per, mine = threadIdx.x % per;
+    const int64_t chunks = p.cols / V, total = p.rows * chunks, t = (int64_t)blockIdx.x * per + mine, all = (int64_t)p.rows * p.cols;
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.0f;
+    if (t < total) {
+        const int each = (p.splits + lanes - 1) / lanes, last = min(p.splits, (lane + 1) * each);
+        const float* src = p.part + t * V;
+#pragma unroll 4
+        for (int s = lane * each; s < last; ++s) {
+            if constexpr (V == 4) {
+                const float4 x = *reinterpret_cast<const float4*>(src + s * all);
+                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+            } else {
+                v[0] += src[s * all];
+            }
+        }
+    }
+    if (lanes > 1) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) sums[threadIdx.x][e] = v[e];
+        __syncthreads();
+        if (lane) return;
+        for (int l = 1; l < lanes; ++l)
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] += sums[threadIdx.x + l * per][e];
+    }
+    if (t >= total) return;
+    const int i = (int)(t / chunks), j = (int)(t - i * chunks) * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        float z = v[e];
+        if constexpr (SPLIT3) {
+            z *= packets::JOIN_SCALE;
+            if (z - z != 0.0f) {
+                const float* a = (const float*)p.a.p + i * p.a.i_step;
+                const float* b = (const float*)p.b.p + (j + e) * p.b.i_step;
+                z = 0.0f;
+                for (int k = 0; k < p.K && z == z; ++k) z = fmaf(a[k * p.a.k_step], b[k * p.b.k_step], z);
+            }
+        }
+        finish<E, O>(p.f, i, j + e, z);
+    }
+}
+
+// How a product is computed: the same answer for the workspace query and for the launch.
+struct GemmPlan {
+    int tile, tiles_i, tiles_j, steps, splits, per_split;
+    double us;
+};
+
+// Tiles of 256, 128 or 64 on a side, the reduction split where tiles alone leave compute units idle: the least expected time. A step of 64 takes a
+// compute unit `step` cycles per tile once enough tiles are there to overlap; alone on it a tile takes `alone`.
+struct TileCost { int tile, resident; double step, alone; };
+constexpr TileCost kTiles[] = {{256, 1, 2400, 2400}, {128, 2, 800, 1100}, {64, 4, 330, 800}};
+GemmPlan plan_gemm(int64_t rows, int64_t cols, int64_t K, int planes) {
+    GemmPlan best{};
+    best.us = 1e30;
+    const int64_t steps = (K + lin::BK - 1) / lin::BK;
+    for (const TileCost& c : kTiles) {
+        const int64_t ti = (rows + c.tile - 1) / c.tile, tj = (cols + c.tile - 1) / c.tile, tiles = ti * tj;
+        if (tiles > 0x7fffffff) continue;
+        for (int64_t want = 1; want <= 1024; want *= 2) {
+            const int64_t most = steps < want ? steps : want, per = (steps + most - 1) / most, splits = (steps + per - 1) / per;
+            if (splits * 2 <= want && want > 1) break;
+            const double part = (splits > 1 || planes > 1) ? 4.0 * splits * rows * cols : 0.0;
+            if (splits > 1 && part > 256e6) break;
+            if (tiles * splits > 0x7fffffff) break;
+            const double all = (double)tiles * splits, rounds = ceil(all / (256.0 * c.resident)), fill = all / 256.0;
+            const double load = fill <= 1.0 ? c.alone : fill >= c.resident ? rounds * c.resident * c.step : fill * c.step > c.alone ? fill * c.step : c.alone;
+            const double us = load * (double)(per * (planes == 3 ? 6 : 1)) / 2.2e3 + (part > 0 ? 4.0 + 2.0 * part / 5e6 : 0.0) + 4.0;
+            if (us < best.us) {
+                best.us = us;
+                best.tile = c.tile; best.tiles_i = (int)ti; best.tiles_j = (int)tj;
+                best.steps = (int)steps; best.splits = (int)splits; best.per_split = (int)per;
+            }
+        }
+    }
+    return best;
+}
+
+int64_t packed_ld(int64_t len) { return (len + 7) / 8 * 8; }
+size_t whole(size_t n) { return (n + 255) / 256 * 256; }
+// bytes of an operand's copy: reduction inner (rows x K) or outer (K x rows)
+size_t packed_bytes(int64_t rows, int64_t K, bool in, int planes) { return whole((size_t)(in ? rows * packed_ld(K) : K * packed_ld(rows)) * 2 * planes); }
+bool whole_packets(int64_t rows, int64_t K, bool in) { return (in ? K : rows) % 8 == 0; }
 
 // g = dy act'(pre), and the sums of its columns over a slice of the rows: a thread per column, rows in order.
 struct ActParams {
@@ -116,24 +219,99 @@ int act_rows(int64_t N, int64_t K) {
 
 }  // namespace
 
-size_t linear_ws_bytes(int64_t, int64_t, int64_t, bool, bool, int) { return 0; }
+size_t linear_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_in, int dtype) {
+    const int planes = dtype == PURINE_F32 ? 3 : 1;
+    const GemmPlan g = plan_gemm(rows, cols, K, planes);
+    size_t n = 0;
+    if (planes == 3 || !whole_packets(rows, K, a_in)) n += packed_bytes(rows, K, a_in, planes);
+    if (planes == 3 || !whole_packets(cols, K, b_in)) n += packed_bytes(cols, K, b_in, planes);
+    if (planes == 3 || g.splits > 1) n += (size_t)g.splits * rows * cols * 4;
+    return n;
+}
 
-hipError_t launch_linear(const LinearCall& c, void*, hipStream_t st) {
-    LinearParams p{};
-    p.a = c.a; p.b = c.b; p.out = c.out; p.bias = c.bias; p.res = c.res; p.pre = c.pre; p.slope = c.slope;
-    p.a_i = c.a_in ? c.a_ld : 1; p.a_k = c.a_in ? 1 : c.a_ld;
-    p.b_i = c.b_in ? c.b_ld : 1; p.b_k = c.b_in ? 1 : c.b_ld;
-    p.out_ld = c.out_ld; p.res_ld = c.res_ld; p.pre_ld = c.pre_ld; p.slope_ld = c.slope_ld;
-    p.rows = (int)c.rows; p.cols = (int)c.cols; p.K = (int)c.K;
-    p.act = c.act; p.accumulate = c.accumulate;
-    p.tiles_j = (int)((c.cols + TS - 1) / TS);
-    const unsigned grid = (unsigned)((c.rows + TS - 1) / TS * p.tiles_j);
-    ProbeScope probe(st);
-    (void)hipGetLastError();
-    if (c.dtype == PURINE_F32) hipLaunchKernelGGL((linear_kernel<float, float>), dim3(grid), dim3(256), 0, st, p);
-    else if (c.out_dtype == PURINE_F32) hipLaunchKernelGGL((linear_kernel<uint16_t, float>), dim3(grid), dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((linear_kernel<uint16_t, uint16_t>), dim3(grid), dim3(256), 0, st, p);
+namespace {
+
+Source source_of(const void* p, int64_t ld, bool in) { return {p, in ? ld : 1, in ? 1 : ld}; }
+
+template <typename E, typename O>
+hipError_t join(const JoinParams& q, hipStream_t st) {
+    JoinParams p = q;
+    const bool v4 = p.cols % 4 == 0;
+    const int64_t threads = (int64_t)p.rows * p.cols / (v4 ? 4 : 1);
+    p.lanes = 1;
+    while (p.lanes < 32 && p.lanes * 4 <= p.splits && threads * p.lanes < 256 * 512) p.lanes *= 2;
+    const int64_t per = 256 / p.lanes, grid = (threads + per - 1) / per;
+    if (v4) hipLaunchKernelGGL((linear_join_kernel<E, O, 4>), dim3((unsigned)grid), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((linear_join_kernel<E, O, 1>), dim3((unsigned)grid), dim3(256), 0, st, p);
     return hipGetLastError();
+}
+
+template <typename T>
+void pack(const void* src, int64_t ld, void* dst, int64_t rows, int64_t K, bool in, hipStream_t st) {
+    const int64_t r = in ? rows : K, len = in ? K : rows, packets = packed_ld(len) / 8, total = r * packets;
+    const unsigned grid = (unsigned)((total + 255) / 256 < 65536 ? (total + 255) / 256 : 65536);
+    hipLaunchKernelGGL((linear_pack_kernel<T>), dim3(grid), dim3(256), 0, st, (const T*)src, ld, (uint16_t*)dst, (int)r, (int)len, (int)packets, r * packets * 16);
+}
+
+}  // namespace
+
+hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
+    const bool f32 = c.dtype == PURINE_F32;
+    const int planes = f32 ? 3 : 1;
+    Finish f{c.bias, c.res, c.pre, c.slope, c.out, c.res_ld, c.pre_ld, c.slope_ld, c.out_ld, c.act, c.accumulate};
+    const Source a = source_of(c.a, c.a_ld, c.a_in), b = source_of(c.b, c.b_ld, c.b_in);
+    (void)hipGetLastError();
+    const int64_t far = (int64_t)1 << 24;
+    if (c.a_ld >= far || c.b_ld >= far) {
+        FarParams p{a, b, f, (int)c.rows, (int)c.cols, (int)c.K, (int)((c.cols + TS - 1) / TS)};
+        const unsigned grid = (unsigned)((c.rows + TS - 1) / TS * p.tiles_j);
+        ProbeScope probe(st);
+        if (f32) hipLaunchKernelGGL((linear_far_kernel<float, float>), dim3(grid), dim3(256), 0, st, p);
+        else if (c.out_dtype == PURINE_F32) hipLaunchKernelGGL((linear_far_kernel<uint16_t, float>), dim3(grid), dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((linear_far_kernel<uint16_t, uint16_t>), dim3(grid), dim3(256), 0, st, p);
+        return hipGetLastError();
+    }
+    GemmPlan g = plan_gemm(c.rows, c.cols, c.K, planes);
+    if (c.a_ld >= far / 4 || c.b_ld >= far / 4) {          // (a tile of 256 rows would span 2^31 bytes)
+        g.tile = 64;
+        g.tiles_i = (int)((c.rows + 63) / 64);
+        g.tiles_j = (int)((c.cols + 63) / 64);
+    }
+    lin::GemmParams p{};
+    char* scratch = (char*)ws;
+    struct Laid { const char* p; int64_t ld, size, plane; };
+    auto lay = [&](const void* src, int64_t ld, int64_t rows, bool in) {
+        if (!f32 && whole_packets(rows, c.K, in)) return Laid{(const char*)src, ld, ((in ? rows : c.K) - 1) * ld * 2 + (in ? c.K : rows) * 2, 0};
+        const Laid l{scratch, packed_ld(in ? c.K : rows), (int64_t)packed_bytes(rows, c.K, in, planes), (in ? rows : c.K) * packed_ld(in ? c.K : rows) * 2};
+        if (f32) pack<float>(src, ld, scratch, rows, c.K, in, st);
+        else pack<uint16_t>(src, ld, scratch, rows, c.K, in, st);
+        scratch += l.size;
+        return l;
+    };
+    const Laid la = lay(c.a, c.a_ld, c.rows, c.a_in), lb = lay(c.b, c.b_ld, c.cols, c.b_in);
+    p.a = la.p; p.a_ld = la.ld; p.a_size = la.size; p.a_plane = la.plane;
+    p.b = lb.p; p.b_ld = lb.ld; p.b_size = lb.size; p.b_plane = lb.plane;
+    p.rows = (int)c.rows; p.cols = (int)c.cols; p.K = (int)c.K;
+    p.planes = planes;
+    p.steps = g.steps; p.per_split = g.per_split; p.splits = g.splits;
+    p.tiles_i = g.tiles_i; p.tiles_j = g.tiles_j;
+    p.group = 8;
+    const bool second = g.splits > 1 || f32;
+    p.part = (float*)scratch;
+    p.out = c.out; p.out_ld = c.out_ld; p.out_f32 = c.out_dtype == PURINE_F32;
+    p.bias = c.bias; p.res = c.res; p.res_ld = c.res_ld; p.pre = c.pre; p.pre_ld = c.pre_ld; p.slope = c.slope; p.slope_ld = c.slope_ld;
+    p.accumulate = c.accumulate;
+    p.vectors = c.out_ld % 8 == 0 && (!c.res || c.res_ld % 8 == 0) && (!c.pre || c.pre_ld % 8 == 0) && (!c.slope || c.slope_ld % 8 == 0);
+    const int act = second ? lin::PART : c.b_in || c.slope ? c.act : PURINE_ACT_NONE;
+    hipError_t e;
+    {
+        ProbeScope probe(st);
+        e = g.tile == 256 ? lin::gemm_256(p, c.a_in, c.b_in, act, st) : g.tile == 128 ? lin::gemm_128(p, c.a_in, c.b_in, act, st) : lin::gemm_64(p, c.a_in, c.b_in, act, st);
+    }
+    if (e != hipSuccess || !second) return e;
+    JoinParams q{p.part, f, a, b, p.rows, p.cols, p.K, p.splits, 1};
+    if (f32) return join<float, float>(q, st);
+    return c.out_dtype == PURINE_F32 ? join<uint16_t, float>(q, st) : join<uint16_t, uint16_t>(q, st);
 }
 
 size_t act_bwd_ws_bytes(int64_t N, int64_t K) {
