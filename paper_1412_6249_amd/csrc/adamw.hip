@@ -179,9 +179,12 @@ __global__ __launch_bounds__(NT) void adamw_kernel(const AdamwParams p) {
         get((const float*)t.m + at, left, m);
         get((const float*)t.v + at, left, v);
     }
+    // Every product and sum of the states is rounded by itself (no fused multiply-add), so that the codes do not depend on how the
+    // formula is evaluated: with bf16 gradients values often lie exactly between two codes.
     float u[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
+#pragma clang fp contract(off)
         const float d = g[i] * p.grad_scale;
         m[i] = p.beta1 * m[i] + p.beta1c * d;
         v[i] = p.beta2 * v[i] + p.beta2c * (d * d);

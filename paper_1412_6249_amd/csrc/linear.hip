@@ -182,39 +182,87 @@ size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 size_t packed_bytes(int64_t rows, int64_t K, bool in, int planes) { return whole((size_t)(in ? rows * packed_ld(K) : K * packed_ld(rows)) * 2 * planes); }
 bool whole_packets(int64_t rows, int64_t K, bool in) { return (in ? K : rows) % 8 == 0; }
 
-// g = dy act'(pre), and the sums of its columns over a slice of the rows: a thread per column, rows in order.
+// g = dy act'(pre), and the sums of its columns over a slice of the rows. Bound: HBM. A thread owns V neighbouring columns (16 bytes where
+// rows are whole packets) and walks down the slice, two rows ahead of their use; the threads of a column join in LDS, the slices in a
+// second kernel, both in order.
 struct ActParams {
     const void* pre; const void* dy; void* g; float* part;
     int64_t pre_ld, dy_ld, g_ld;
-    int N, K, rows, act;
+    int N, K, rows, slices, tiles;
 };
-template <typename T>
-__global__ __launch_bounds__(256) void act_bwd_kernel(const ActParams p) {
-    const int tiles = (p.K + 255) / 256, slice = blockIdx.x / tiles, j = (int)(blockIdx.x % tiles) * 256 + threadIdx.x;
-    if (j >= p.K) return;
-    float sum = 0.0f;
-    for (int64_t i = (int64_t)slice * p.rows; i < min((int64_t)(slice + 1) * p.rows, (int64_t)p.N); ++i) {
-        float v = widen<T>(((const T*)p.dy)[i * p.dy_ld + j]);
-        if (p.pre) v *= slope_any(p.act, widen<T>(((const T*)p.pre)[i * p.pre_ld + j]));
-        if (p.g) narrow(v, (T*)p.g + i * p.g_ld + j);
-        sum += v;
+constexpr int ANT = 256;
+template <typename T, int V, int ACT>
+__global__ __launch_bounds__(ANT) void act_bwd_kernel(const ActParams p) {
+    __shared__ float sums[ANT * V];
+    const int slice = blockIdx.x / p.tiles, first = (int)(blockIdx.x - (unsigned)slice * p.tiles) * ANT;
+    const int tile = min(ANT, p.K / V - first), R = ANT / tile, r = threadIdx.x / tile, j = (first + (int)threadIdx.x % tile) * V;
+    const int i1 = min((slice + 1) * p.rows, p.N);
+    float sum[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = 0.0f;
+    if (r < R) {
+        const T* dy = (const T*)p.dy + j;
+        const T* pre = (const T*)p.pre + j;
+        T* g = (T*)p.g + j;
+        constexpr int AHEAD = 4;
+        for (int i = slice * p.rows + r; i < i1; i += R * AHEAD) {
+            float v[AHEAD][V], z[AHEAD][V];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t row = min(i + u * R, i1 - 1);
+                lin::get_v(dy + row * p.dy_ld, v[u]);
+                if (ACT != PURINE_ACT_NONE) lin::get_v(pre + row * p.pre_ld, z[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t row = i + u * R;
+                if (row >= i1) break;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    if (ACT != PURINE_ACT_NONE) v[u][e] *= act_slope<ACT>(z[u][e]);
+                    sum[e] += v[u][e];
+                }
+                if (p.g) lin::put_v(g + row * p.g_ld, v[u]);
+            }
+        }
     }
-    if (p.part) p.part[(size_t)slice * p.K + j] = sum;
+    if (!p.part) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) sums[threadIdx.x * V + e] = sum[e];
+    __syncthreads();
+    if (r) return;
+    for (int k = 1; k < R; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[e] += sums[(threadIdx.x + k * tile) * V + e];
+    float* o = p.part + (size_t)slice * p.K + j;
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = sum[e];
 }
+// 16 columns per workgroup, the slices over 16 threads each.
 template <typename O>
 __global__ __launch_bounds__(256) void column_sums_kernel(const float* part, O* db, int slices, int K, int accumulate) {
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j >= K) return;
+    __shared__ float sums[16][17];
+    const int l = threadIdx.x & 15, r = threadIdx.x >> 4, j = blockIdx.x * 16 + l;
     float sum = 0.0f;
-    for (int s = 0; s < slices; ++s) sum += part[(size_t)s * K + j];
+    if (j < K) {
+#pragma unroll 4
+        for (int s = r; s < slices; s += 16) sum += part[(size_t)s * K + j];
+    }
+    sums[r][l] = sum;
+    __syncthreads();
+    if (r || j >= K) return;
+    for (int k = 1; k < 16; ++k) sum += sums[k][l];
     if (accumulate) sum += widen<O>(db[j]);
     narrow(sum, db + j);
 }
+// Rows of a slice: some 1024 workgroups, and few enough slices that their sums are a small part of the matrix; 16 rows per thread at least.
 int act_rows(int64_t N, int64_t K) {
-    int64_t tiles = (K + 255) / 256, slices = 1024 / tiles;
+    const int64_t vectors = (K + 7) / 8, tiles = (vectors + ANT - 1) / ANT, R = vectors < ANT ? ANT / vectors : 1;
+    int64_t slices = 1024 / tiles;
     if (slices < 1) slices = 1;
     int64_t rows = (N + slices - 1) / slices;
-    return (int)(rows < 16 ? 16 : rows);
+    if (rows < 8 * R) rows = 8 * R;
+    return (int)(rows < N ? rows : N);
 }
 
 }  // namespace
@@ -319,20 +367,39 @@ size_t act_bwd_ws_bytes(int64_t N, int64_t K) {
     return (size_t)slices * K * 4;
 }
 
+namespace {
+template <typename T, int V>
+void act_bwd(const ActParams& q, int act, hipStream_t st) {
+    ActParams p = q;
+    p.tiles = (p.K / V + ANT - 1) / ANT;
+    const unsigned grid = (unsigned)((int64_t)p.slices * p.tiles);
+    switch (act) {
+        case PURINE_ACT_RELU: hipLaunchKernelGGL((act_bwd_kernel<T, V, PURINE_ACT_RELU>), dim3(grid), dim3(ANT), 0, st, p); break;
+        case PURINE_ACT_SILU: hipLaunchKernelGGL((act_bwd_kernel<T, V, PURINE_ACT_SILU>), dim3(grid), dim3(ANT), 0, st, p); break;
+        case PURINE_ACT_GELU: hipLaunchKernelGGL((act_bwd_kernel<T, V, PURINE_ACT_GELU>), dim3(grid), dim3(ANT), 0, st, p); break;
+        case PURINE_ACT_GELU_TANH: hipLaunchKernelGGL((act_bwd_kernel<T, V, PURINE_ACT_GELU_TANH>), dim3(grid), dim3(ANT), 0, st, p); break;
+        default: hipLaunchKernelGGL((act_bwd_kernel<T, V, PURINE_ACT_NONE>), dim3(grid), dim3(ANT), 0, st, p); break;
+    }
+}
+}  // namespace
+
 hipError_t launch_act_bwd(int dtype, const void* pre, int64_t pre_ld, const void* dy, int64_t dy_ld, void* g, int64_t g_ld, void* db, int db_dtype,
                           bool accumulate, int64_t N, int64_t K, int act, void* ws, hipStream_t st) {
-    ActParams p{pre, dy, g, db ? (float*)ws : nullptr, pre_ld, dy_ld, g_ld, (int)N, (int)K, act_rows(N, K), act};
-    const int slices = (int)((N + p.rows - 1) / p.rows), tiles = (int)((K + 255) / 256);
+    ActParams p{pre, dy, g, db ? (float*)ws : nullptr, pre_ld, dy_ld, g_ld, (int)N, (int)K, act_rows(N, K), 0, 1};
+    p.slices = (int)((N + p.rows - 1) / p.rows);
+    if (!pre) act = PURINE_ACT_NONE;
+    const int64_t all = K | dy_ld | (pre ? pre_ld : 0) | (g ? g_ld : 0);
     (void)hipGetLastError();
     {
         ProbeScope probe(st);
-        if (dtype == PURINE_F32) hipLaunchKernelGGL((act_bwd_kernel<float>), dim3((unsigned)(slices * (int64_t)tiles)), dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((act_bwd_kernel<uint16_t>), dim3((unsigned)(slices * (int64_t)tiles)), dim3(256), 0, st, p);
+        if (dtype == PURINE_F32) all % 4 == 0 ? act_bwd<float, 4>(p, act, st) : act_bwd<float, 1>(p, act, st);
+        else all % 8 == 0 ? act_bwd<uint16_t, 8>(p, act, st) : act_bwd<uint16_t, 1>(p, act, st);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !db) return e;
-    if (db_dtype == PURINE_F32) hipLaunchKernelGGL((column_sums_kernel<float>), dim3(tiles), dim3(256), 0, st, p.part, (float*)db, slices, (int)K, accumulate);
-    else hipLaunchKernelGGL((column_sums_kernel<uint16_t>), dim3(tiles), dim3(256), 0, st, p.part, (uint16_t*)db, slices, (int)K, accumulate);
+    const unsigned grid = (unsigned)((K + 15) / 16);
+    if (db_dtype == PURINE_F32) hipLaunchKernelGGL((column_sums_kernel<float>), dim3(grid), dim3(256), 0, st, p.part, (float*)db, p.slices, (int)K, accumulate);
+    else hipLaunchKernelGGL((column_sums_kernel<uint16_t>), dim3(grid), dim3(256), 0, st, p.part, (uint16_t*)db, p.slices, (int)K, accumulate);
     return hipGetLastError();
 }
 

@@ -241,6 +241,22 @@ __device__ __forceinline__ void put8(float* p, bool whole, int n, const float (&
     }
 }
 
+// V neighbouring values: 16 bytes or one.
+template <typename T, int V>
+__device__ __forceinline__ void get_v(const T* p, float (&v)[V]) {
+    if constexpr (V == 8) get8(p, true, 8, v);
+    else if constexpr (V == 4) { const floatx4 k = *reinterpret_cast<const floatx4*>(p); v[0] = k[0]; v[1] = k[1]; v[2] = k[2]; v[3] = k[3]; }
+    else if constexpr (sizeof(T) == 2) v[0] = bf2f(p[0]);
+    else v[0] = p[0];
+}
+template <typename T, int V>
+__device__ __forceinline__ void put_v(T* p, const float (&v)[V]) {
+    if constexpr (V == 8) put8(p, true, 8, v);
+    else if constexpr (V == 4) *reinterpret_cast<floatx4*>(p) = floatx4{v[0], v[1], v[2], v[3]};
+    else if constexpr (sizeof(T) == 2) p[0] = f2bf(v[0]);
+    else p[0] = v[0];
+}
+
 // The tile of a workgroup: consecutive workgroups go to the eight dies in turn, so a die takes a consecutive eighth of the tiles;
 // there, `group` row tiles go through the column tiles together.
 __device__ __forceinline__ void tile_of(const GemmParams& p, int& ti, int& tj, int& split) {

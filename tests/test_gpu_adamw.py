@@ -1,9 +1,10 @@
 """The AdamW step against its definition in 64 bits: fp32 states, 8-bit states (decoded, stepped and encoded in plain torch operations of the
 same formulas), tensors of one element, of a block, of a workgroup and one beside them, more tensors than a launch holds, every type.
 
-Bounds. fp32: about ten roundings of 2^-24 on w, three on the states: 16 eps. bf16 weights: one rounding, 2^-8 of the value. 8-bit codes: a value in
-steps of its codes (16 at most) is known to 1e-6 of itself, so that a code may differ, by one place, only where that number plus the threshold
-is within 2e-5 of a whole one. (With bf16 gradients such ties are common: 0.9 and 0.07 of small binary numbers add up to whole halves.)"""
+Bounds. fp32: about ten roundings of 2^-24 on w, three on the states: 16 eps. bf16 weights: one rounding, 2^-8 of the value. 8-bit codes: m
+is known to 4 eps of the terms that it is made of, sqrt(v) to 4 eps of itself, so that a code may differ, by one place, only where the value
+in steps of its codes plus the threshold is that near to a whole number (and 32 eps, the sum's own rounding). With bf16 gradients such ties are
+common: 0.9 and 0.07 of small binary numbers add up to whole halves."""
 import math
 
 import pytest
@@ -70,7 +71,7 @@ def _thresholds(n, tensor, seed, step):
     return [((b & 255).double() + 0.5) / 256 for b in (h, h >> 8)]
 
 
-def _encode(x, d, floor):
+def _encode(x, d, floor, unsure=0.0):
     """Codes' values (in scales) and scales, in 64 bits on the CPU."""
     n = x.numel()
     pad = torch.zeros(_blocks(n) * BLOCK, dtype=torch.float64)
@@ -82,7 +83,8 @@ def _encode(x, d, floor):
     z = torch.where(scale[:, None] > 0, a / scale.clamp(min=2.0 ** -120)[:, None], torch.zeros_like(a)).reshape(-1)[:n]
     step = 2.0 ** (torch.floor(torch.log2(z.clamp(min=2.0 ** -30))).clamp(min=-6) - 3)
     place = z / step + d
-    near = (place - place.round()).abs() < 2e-5
+    doubt = torch.as_tensor(unsure, dtype=torch.float64).cpu() / (scale.clamp(min=2.0 ** -120).repeat_interleave(BLOCK)[:n] * step)
+    near = (place - place.round()).abs() <= doubt + 32 * EPS
     q = torch.floor(place) * step
     if floor:
         q = torch.where(z > 0, q.clamp(min=2.0 ** -9), q)
@@ -129,8 +131,8 @@ def test_8_bit_states(types, dither):
         assert bool(((w[i].double() - ww).abs() <= (2 ** -8 if "w16" in types else 16 * EPS) * ((ww - w0[i]).abs() + w0[i].abs())).all()), i
         assert torch.equal(copy[i], w[i].to(torch.bfloat16))
         dm, dv = _thresholds(n, i, seed, step) if dither else (0.5, 0.5)
-        for key, x, d, floor in (("m", wm, dm, False), ("v", wv.sqrt(), dv, True)):
-            q, scale, near = _encode(x, d, floor)
+        for key, x, d, floor, terms in (("m", wm, dm, False, wm.abs() + m0[i].abs()), ("v", wv.sqrt(), dv, True, wv.sqrt())):
+            q, scale, near = _encode(x, d, floor, 4 * EPS * terms)
             assert torch.equal(s[key + "_scale"][i].cpu().double(), scale), (key, i)
             off = (s[key][i].float().cpu().double() - q).abs()
             assert bool((off <= 0.1251 * q.abs() + 2.0 ** -9).all())
