@@ -72,14 +72,15 @@ template <int R, bool IN, bool DEALT, int SKEW>
 struct Operand {
     typedef Stage<R, IN, SKEW> S;
     static constexpr int LOADS = S::UNITS / 4;
-    unsigned off[LOADS];                   // bytes from the step's base
-    int k_at[LOADS];                       // first k of the packet (IN) or its k
-    const char* base;                      // of the current step's first plane
+    unsigned off[LOADS];                   // bytes of this lane's packets from the step's base ...
+    unsigned now[LOADS];                   // ... or NOWHERE past the reduction's end
+    int k_at;                              // first k of the first packet (IN: of all)
+    const char* base;
     const char* end;
     int64_t k_bytes;                       // per step
     int frag;                              // LDS bytes of this lane's first fragment
 
-    __device__ void init(const char* p, int64_t size, int64_t ld, int first, int limit, int lane, int wave) {
+    __device__ __forceinline__ void init(const char* p, int64_t size, int64_t ld, int first, int limit, int lane, int wave) {
         base = p + (IN ? first * ld * 2 : (int64_t)first * 2);
         end = p + size;
         k_bytes = IN ? BK * 2 : BK * ld * 2;
@@ -87,14 +88,15 @@ struct Operand {
         for (int u = 0; u < LOADS; ++u) {
             const int unit = u * 4 + wave;
             if constexpr (IN) {
-                const int row = unit * 8 + (lane >> 3), c = (lane & 7) ^ exchange<DEALT>(row);
+                const int row = unit * 8 + (lane >> 3), c = (lane & 7) ^ exchange<DEALT>(row);      // (the same c for every u)
                 off[u] = (unsigned)(min(row, limit - first - 1) * ld * 2) + c * 16;      // (rows past the last read it again)
-                k_at[u] = c * 8;
+                if (u == 0) k_at = c * 8;
             } else {
                 const int k = unit + lane / S::PER_ROW * S::UNITS, c = min(lane % S::PER_ROW, (limit - first - 1) / 8);
                 off[u] = (unsigned)(k * ld * 2) + c * 16;
-                k_at[u] = k;
+                if (u == 0) k_at = k;
             }
+            now[u] = off[u];
         }
         const int r = lane & 15, q = lane >> 4;
         if constexpr (IN) {
@@ -105,15 +107,15 @@ struct Operand {
             frag = (k % S::UNITS) * S::UNIT + (k / S::UNITS) * (R * 2) + (DEALT ? 8 * (r & 3) : 4 * (r & 3)) * 2;
         }
     }
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const char* at) const {
-        const int64_t room = end - at;
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), (short)0, (int)(room < 0x7fffffff ? room : 0x7fffffff), 0x00020000);
+    // only the first `left` elements of a step exist
+    __device__ __forceinline__ void mask(int left) {
+#pragma unroll
+        for (int u = 0; u < LOADS; ++u) now[u] = k_at + (IN ? 0 : 4 * u) < left ? off[u] : NOWHERE;
     }
-    // one load of a step's tile; `left` elements of the reduction remain from the step's first on
-    template <int U>
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, unsigned char* lds, int wave, int left) const {
-        const unsigned o = k_at[U] < left ? off[U] : NOWHERE;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (U * 4 + wave) * S::UNIT), 16, o, 0, 0, 0);
+    __device__ __forceinline__ u32x4 resource(const char* at) const {
+        const int64_t room = end - at;
+        const uint64_t p = (uint64_t)(uintptr_t)at;
+        return u32x4{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, room < 0x7fffffff ? (uint32_t)room : 0x7fffffffu, 0x00020000u};
     }
     // LDS offset of tile t (16 rows) from this lane's first fragment
     static constexpr int tile_at(int t) {
@@ -128,7 +130,7 @@ struct Operand {
 // One fragment's read. The wait is at the end of the same asm block (see block()).
 #define LIN_READ_IN(F, AT, OFF) "ds_read_b128 " F ", " AT " offset:" OFF "\n\t"
 #define LIN_READ_OUT(LO, HI, AT, OFF, OFF2) "ds_read_b64_tr_b16 " LO ", " AT " offset:" OFF "\n\tds_read_b64_tr_b16 " HI ", " AT " offset:" OFF2 "\n\t"
-#define LIN_MFMA(ACC, B) "v_mfma_f32_16x16x32_bf16 " ACC ", " B ", %[a], " ACC "\n\t"
+#define LIN_WAIT "s_waitcnt lgkmcnt(0)"
 
 // A fragment as it is read: 16 bytes, or two times 8.
 template <bool IN> struct Frag { bf16x8 v; };
@@ -145,41 +147,71 @@ struct Shape {
     static constexpr int TI = BI / 32, TJ = BJ / 32;
 };
 
-// Multiplies a row tile with every column tile, and reads tile I of both operands for the half step after: the reads have the MFMAs'
-// time before the wait at the end of the same asm block, so that no read is in flight that the compiler does not know of.
-#define LIN_ACC2 [c0] "+a"(c[0]), [c1] "+a"(c[1])
-#define LIN_ACC4 LIN_ACC2, [c2] "+a"(c[2]), [c3] "+a"(c[3])
-#define LIN_ACC8 LIN_ACC4, [c4] "+a"(c[4]), [c5] "+a"(c[5]), [c6] "+a"(c[6]), [c7] "+a"(c[7])
-#define LIN_B2 [b0] "v"(b[0]), [b1] "v"(b[1])
-#define LIN_B4 LIN_B2, [b2] "v"(b[2]), [b3] "v"(b[3])
-#define LIN_B8 LIN_B4, [b4] "v"(b[4]), [b5] "v"(b[5]), [b6] "v"(b[6]), [b7] "v"(b[7])
-#define LIN_M2 LIN_MFMA("%[c0]", "%[b0]") LIN_MFMA("%[c1]", "%[b1]")
-#define LIN_M4 LIN_M2 LIN_MFMA("%[c2]", "%[b2]") LIN_MFMA("%[c3]", "%[b3]")
-#define LIN_M8 LIN_M4 LIN_MFMA("%[c4]", "%[b4]") LIN_MFMA("%[c5]", "%[b5]") LIN_MFMA("%[c6]", "%[b6]") LIN_MFMA("%[c7]", "%[b7]")
-#define LIN_WAIT "s_waitcnt lgkmcnt(0)"
-#define LIN_BLOCK(M, ACC, B)                                                                                                                   \
-    if constexpr (AIN && BIN)                                                                                                              \
-            asm volatile(LIN_READ_IN("%[na]", "%[pa]", "%[ao]") LIN_READ_IN("%[nb]", "%[pb]", "%[bo]") M LIN_WAIT                              \
-                         : ACC, [na] "=&v"(na.v), [nb] "=&v"(nb.v)                                                                             \
-                         : B, [a] "v"(a), [pa] "v"(a_at), [pb] "v"(b_at), [ao] "n"(ao), [bo] "n"(bo) : "memory");                              \
-        else if constexpr (AIN)                                                                                                                \
-            asm volatile(LIN_READ_IN("%[na]", "%[pa]", "%[ao]") LIN_READ_OUT("%[nl]", "%[nh]", "%[pb]", "%[bo]", "%[bh]") M LIN_WAIT           \
-                         : ACC, [na] "=&v"(na.v), [nl] "=&v"(nb.lo), [nh] "=&v"(nb.hi)                                                         \
-                         : B, [a] "v"(a), [pa] "v"(a_at), [pb] "v"(b_at), [ao] "n"(ao), [bo] "n"(bo), [bh] "n"(bh) : "memory");                \
-        else                                                                                                                                   \
-            asm volatile(LIN_READ_OUT("%[al]", "%[ahi]", "%[pa]", "%[ao]", "%[ah]") LIN_READ_OUT("%[nl]", "%[nh]", "%[pb]", "%[bo]", "%[bh]") M LIN_WAIT \
-                         : ACC, [al] "=&v"(na.lo), [ahi] "=&v"(na.hi), [nl] "=&v"(nb.lo), [nh] "=&v"(nb.hi)                                    \
-                         : B, [a] "v"(a), [pa] "v"(a_at), [pb] "v"(b_at), [ao] "n"(ao), [ah] "n"(ah), [bo] "n"(bo), [bh] "n"(bh) : "memory")
-template <typename T, bool AIN, bool BIN, int I, int TJ>
-__device__ __forceinline__ void block(floatx4 (&c)[TJ], const Frag<AIN>& fa, const Frag<BIN> (&fb)[TJ], Frag<AIN>& na, Frag<BIN>& nb, int a_at, int b_at) {
-    constexpr int ao = T::A::tile_at(I), bo = T::B::tile_at(I), ah = ao + T::A::HALF, bh = bo + T::B::HALF;
+// One asm block multiplies two row tiles from I on with every column tile. Between its MFMAs, in whose 16 cycles other instructions issue for nothing,
+// it reads two tiles of both operands for the half step after, and (LOAD) requests a part of a later step's tiles. The reads have
+// the remaining MFMAs' time before the wait at the block's end, so that no read is in flight that the compiler does not know of;
+// the requests fill no register, and meet() waits for them. (8192 x 4096 x 8192 with these in front of the MFMAs instead: data gradient 401 us,
+// with a block for each row tile besides: LDS reads take longer than 128 cycles beside three other wavefronts'.)
+#define LIN_C2(N, R) [N##0] "+a"(c[R][0]), [N##1] "+a"(c[R][1])
+#define LIN_C4(N, R) LIN_C2(N, R), [N##2] "+a"(c[R][2]), [N##3] "+a"(c[R][3])
+#define LIN_C8(N, R) LIN_C4(N, R), [N##4] "+a"(c[R][4]), [N##5] "+a"(c[R][5]), [N##6] "+a"(c[R][6]), [N##7] "+a"(c[R][7])
+#define LIN_B2() [b0] "v"(b[0]), [b1] "v"(b[1])
+#define LIN_B4() LIN_B2(), [b2] "v"(b[2]), [b3] "v"(b[3])
+#define LIN_B8() LIN_B4(), [b4] "v"(b[4]), [b5] "v"(b[5]), [b6] "v"(b[6]), [b7] "v"(b[7])
+#define LIN_M(N, J, A) "v_mfma_f32_16x16x32_bf16 %[" #N #J "], %[b" #J "], %[" #A "], %[" #N #J "]\n\t"
+// a request: where in LDS, an instruction between, the load
+#define LIN_TO(K) "s_mov_b32 m0, %[m" #K "]\n\t"
+#define LIN_GET(K) "buffer_load_dwordx4 %[v" #K "], %[r" #K "], 0 offen lds\n\t"
+#define LIN_NO(K) ""
+// the MFMAs of a block of 2 x 8, 2 x 4 or 2 x 2 tiles, with the reads R0..R3 and the requests
+#define LIN_SEQ8(R0, R1, R2, R3, T, G) LIN_M(c, 0, a0) R0 LIN_M(c, 1, a0) R1 LIN_M(c, 2, a0) R2 LIN_M(c, 3, a0) R3 T(0) LIN_M(c, 4, a0) G(0) LIN_M(c, 5, a0) T(1) \
+    LIN_M(c, 6, a0) G(1) LIN_M(c, 7, a0) T(2) LIN_M(d, 0, a1) G(2) LIN_M(d, 1, a1) T(3) LIN_M(d, 2, a1) G(3) LIN_M(d, 3, a1) LIN_M(d, 4, a1) LIN_M(d, 5, a1)     \
+    LIN_M(d, 6, a1) LIN_M(d, 7, a1)
+#define LIN_SEQ4(R0, R1, R2, R3, T, G) LIN_M(c, 0, a0) R0 R1 LIN_M(c, 1, a0) R2 R3 T(0) LIN_M(c, 2, a0) G(0) T(1) LIN_M(c, 3, a0) G(1) T(2) LIN_M(d, 0, a1) G(2) T(3) \
+    LIN_M(d, 1, a1) G(3) LIN_M(d, 2, a1) LIN_M(d, 3, a1)
+#define LIN_SEQ2(R0, R1, R2, R3, T, G) R0 R1 R2 R3 T(0) LIN_M(c, 0, a0) G(0) T(1) LIN_M(c, 1, a0) G(1) T(2) LIN_M(d, 0, a1) G(2) T(3) LIN_M(d, 1, a1) G(3)
+// operand X (a or b), tile number R of the block: reading it, what it is read to, where from
+#define LIN_IN(X, R) LIN_READ_IN("%[n" #X #R "]", "%[p" #X "]", "%[o" #X #R "]")
+#define LIN_OUT(X, R) LIN_READ_OUT("%[n" #X #R "]", "%[h" #X #R "]", "%[p" #X "]", "%[o" #X #R "]", "%[q" #X #R "]")
+#define LIN_IN_D(X, R, F) [n##X##R] "=&v"(F[I + R].v)
+#define LIN_OUT_D(X, R, F) [n##X##R] "=&v"(F[I + R].lo), [h##X##R] "=&v"(F[I + R].hi)
+#define LIN_IN_O(X, O, R) [o##X##R] "n"(O::tile_at(I + R))
+#define LIN_OUT_O(X, O, R) [o##X##R] "n"(O::tile_at(I + R)), [q##X##R] "n"(O::tile_at(I + R) + O::HALF)
+#define LIN_REQ(K) [m##K] "s"(q[K].to), [v##K] "v"(q[K].off), [r##K] "s"(q[K].from)
+#define LIN_ASM(X, Y, SEQ, C, B)                                                                                                               \
+    if constexpr (LOAD)                                                                                                                        \
+        asm volatile(SEQ(LIN_##X(a, 0), LIN_##Y(b, 0), LIN_##X(a, 1), LIN_##Y(b, 1), LIN_TO, LIN_GET) LIN_WAIT                                 \
+                     : C(c, I), C(d, I + 1), LIN_##X##_D(a, 0, na), LIN_##X##_D(a, 1, na), LIN_##Y##_D(b, 0, nb), LIN_##Y##_D(b, 1, nb)        \
+                     : B(), [a0] "v"(a[0]), [a1] "v"(a[1]), [pa] "v"(a_at), [pb] "v"(b_at), LIN_##X##_O(a, A, 0), LIN_##X##_O(a, A, 1),          \
+                       LIN_##Y##_O(b, O, 0), LIN_##Y##_O(b, O, 1), LIN_REQ(0), LIN_REQ(1), LIN_REQ(2), LIN_REQ(3) : "memory");           \
+    else                                                                                                                                       \
+        asm volatile(SEQ(LIN_##X(a, 0), LIN_##Y(b, 0), LIN_##X(a, 1), LIN_##Y(b, 1), LIN_NO, LIN_NO) LIN_WAIT                                  \
+                     : C(c, I), C(d, I + 1), LIN_##X##_D(a, 0, na), LIN_##X##_D(a, 1, na), LIN_##Y##_D(b, 0, nb), LIN_##Y##_D(b, 1, nb)        \
+                     : B(), [a0] "v"(a[0]), [a1] "v"(a[1]), [pa] "v"(a_at), [pb] "v"(b_at), LIN_##X##_O(a, A, 0), LIN_##X##_O(a, A, 1),          \
+                       LIN_##Y##_O(b, O, 0), LIN_##Y##_O(b, O, 1) : "memory")
+#define LIN_BLOCK(SEQ, C, B)                                      \
+    if constexpr (AIN && BIN) { LIN_ASM(IN, IN, SEQ, C, B); }     \
+    else if constexpr (AIN) { LIN_ASM(IN, OUT, SEQ, C, B); }      \
+    else { LIN_ASM(OUT, OUT, SEQ, C, B); }
+
+// A 1024-byte load: LDS address, this lane's offset, the buffer. (M0 is the asm blocks' own here: nothing else in the kernel uses it.)
+struct Request { int to; unsigned off; u32x4 from; };
+__device__ __forceinline__ void request_now(const Request& q) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(q.to), "v"(q.off), "s"(q.from) : "memory");
+}
+
+template <typename T, bool AIN, bool BIN, bool LOAD, int I, int TI, int TJ>
+__device__ __forceinline__ void block(floatx4 (&c)[TI][TJ], const Frag<AIN> (&fa)[TI], const Frag<BIN> (&fb)[TJ], Frag<AIN> (&na)[TI], Frag<BIN> (&nb)[TJ], int a_at,
+                                      int b_at, const Request (&q)[4]) {
+    typedef typename T::A A;
+    typedef typename T::B O;
     bf16x8 b[TJ];
 #pragma unroll
     for (int j = 0; j < TJ; ++j) b[j] = value(fb[j]);
-    const bf16x8 a = value(fa);
-    if constexpr (TJ == 8) { LIN_BLOCK(LIN_M8, LIN_ACC8, LIN_B8); }
-    else if constexpr (TJ == 4) { LIN_BLOCK(LIN_M4, LIN_ACC4, LIN_B4); }
-    else { LIN_BLOCK(LIN_M2, LIN_ACC2, LIN_B2); }
+    const bf16x8 a[2] = {value(fa[I]), value(fa[I + 1])};
+    if constexpr (TJ == 8) { LIN_BLOCK(LIN_SEQ8, LIN_C8, LIN_B8) }
+    else if constexpr (TJ == 4) { LIN_BLOCK(LIN_SEQ4, LIN_C4, LIN_B4) }
+    else { LIN_BLOCK(LIN_SEQ2, LIN_C2, LIN_B2) }
 }
 // One fragment, waited for.
 template <int OFF, int>
@@ -190,11 +222,11 @@ __device__ __forceinline__ void read_now(Frag<false>& f, int at) {
 }
 // A lane's write of an accumulator and the MFMA that reads it, and the other way round, want some cycles between them, which the
 // compiler does not see to: it does not know these MFMAs.
-template <int TJ>
-__device__ __forceinline__ void settle(floatx4 (&c)[TJ]) {
-    if constexpr (TJ == 8) asm volatile("s_nop 15\n\ts_nop 15" : LIN_ACC8);
-    else if constexpr (TJ == 4) asm volatile("s_nop 15\n\ts_nop 15" : LIN_ACC4);
-    else asm volatile("s_nop 15\n\ts_nop 15" : LIN_ACC2);
+template <int I, int TI, int TJ>
+__device__ __forceinline__ void settle(floatx4 (&c)[TI][TJ]) {
+    if constexpr (TJ == 8) asm volatile("s_nop 15\n\ts_nop 15" : LIN_C8(c, I));
+    else if constexpr (TJ == 4) asm volatile("s_nop 15\n\ts_nop 15" : LIN_C4(c, I));
+    else asm volatile("s_nop 15\n\ts_nop 15" : LIN_C2(c, I));
 }
 
 // Eight values of a row, from and to memory: whole (16-byte aligned), or those of the first `n`.
@@ -298,20 +330,27 @@ __global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear
     const char *a_next = A.base + s0 * A.k_bytes, *b_next = B.base + s0 * B.k_bytes;
     const char *const a_first = a_next, *const b_first = b_next;
     if (p.planes != 1) { a_next += p.a_plane; b_next += p.b_plane; }
-    // (always as many loads, so that the loop has no branches; past the end they fetch nothing)
-    int room = 0;
-    unsigned char* to = smem;
-    __amdgpu_buffer_rsrc_t ra, rb;
+    const int lds = (int)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+    constexpr int LOADS = T::A::LOADS + T::B::LOADS;
+    // (always as many loads; past the end they fetch nothing)
+    int to = 0;
+    bool masked = false;
+    u32x4 ra, rb;
     auto begin_request = [&](int buf) {
-        room = left > 0 ? p.K - k_next * BK : 0;
-        to = smem + buf * T::STAGE;
+        const int room = left > 0 ? p.K - k_next * BK : 0;
+        if (room < BK || masked) {
+            A.mask(room);
+            B.mask(room);
+            masked = room < BK;
+        }
+        to = lds + buf * T::STAGE;
         ra = A.resource(a_next);
         rb = B.resource(b_next);
     };
-    auto request_one = [&](auto K) {
+    auto request_of = [&](auto K) {
         constexpr int k = K.value;
-        if constexpr (k < T::A::LOADS) A.template load<k>(ra, to, wave, room);
-        else B.template load<k - T::A::LOADS>(rb, to + T::A_BYTES, wave, room);
+        if constexpr (k < T::A::LOADS) return Request{to + (k * 4 + wave) * T::A::S::UNIT, A.now[k], ra};
+        else return Request{to + T::A_BYTES + ((k - T::A::LOADS) * 4 + wave) * T::B::S::UNIT, B.now[k - T::A::LOADS], rb};
     };
     auto end_request = [&]() {
         --left;
@@ -330,7 +369,7 @@ __global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear
     };
     auto request = [&](int buf) {
         begin_request(buf);
-        each<T::A::LOADS + T::B::LOADS>(request_one);
+        each<LOADS>([&](auto K) { request_now(request_of(K)); });
         end_request();
     };
 
@@ -350,7 +389,6 @@ __global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    const int lds = (int)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
     auto a_at = [&](int buf, int kk) { return lds + buf * T::STAGE + T::A::half_at(a_frag, kk); };
     auto b_at = [&](int buf, int kk) { return lds + buf * T::STAGE + T::A_BYTES + T::B::half_at(b_frag, kk); };
 
@@ -360,85 +398,106 @@ __global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear
     each<TI>([&](auto I) {
         read_now<T::A::tile_at(I.value), T::A::HALF>(fa[0][I.value], a_at(0, 0));
         read_now<T::B::tile_at(I.value), T::B::HALF>(fb[0][I.value], b_at(0, 0));
-        settle(acc[I.value]);
+        settle<I.value>(acc);
     });
     for (int s = 0, buf = 0; s < total; ++s, buf ^= 1) {
         const int a1 = a_at(buf, 1), b1 = b_at(buf, 1), a0 = a_at(buf ^ 1, 0), b0 = b_at(buf ^ 1, 0);
-        each<TI>([&](auto I) {
-            constexpr int i = I.value;
-            block<T, AIN, BIN, i>(acc[i], fa[0][i], fb[0], fa[1][i], fb[1][i], a1, b1);
-        });
+        const Request none[4] = {};
+        each<TI / 2>([&](auto I) { block<T, AIN, BIN, false, 2 * I.value>(acc, fa[0], fb[0], fa[1], fb[1], a1, b1, none); });
         meet();                                    // step s + 1 is in the other buffer, and nobody reads this one any more
         begin_request(buf);
-        each<TI>([&](auto I) {
-            constexpr int i = I.value, n = (T::A::LOADS + T::B::LOADS) / TI;
-            each<n>([&](auto K) { request_one(std::integral_constant<int, i * n + K.value>()); });
-            block<T, AIN, BIN, i>(acc[i], fa[1][i], fb[1], fa[0][i], fb[0][i], a0, b0);
+        each<TI / 2>([&](auto I) {
+            constexpr int i = 4 * I.value;
+            static_assert(LOADS == TI / 2 * 4, "four requests in every block");
+            const Request q[4] = {request_of(std::integral_constant<int, i>()), request_of(std::integral_constant<int, i + 1>()),
+                                  request_of(std::integral_constant<int, i + 2>()), request_of(std::integral_constant<int, i + 3>())};
+            block<T, AIN, BIN, true, 2 * I.value>(acc, fa[1], fb[1], fa[0], fb[0], a0, b0, q);
         });
         end_request();
     }
-    each<TI>([&](auto I) { settle(acc[I.value]); });
-    // (the loads past the end write zeros into LDS: they are over before the workgroup's LDS is another's)
-    __builtin_amdgcn_s_waitcnt(0x0070);
+    each<TI>([&](auto I) { settle<I.value>(acc); });
+    meet();                                        // (the loads past the end wrote zeros) LDS is free
 
-    // results: row i0 + wi * BI / 2 + i * 16 + (lane & 15), eight columns from j0 + wj * BJ / 2 + pair * 32 + (lane >> 4) * 8
-    const int row0 = i0 + wi * (BI / 2) + (lane & 15), col0 = j0 + wj * (BJ / 2) + (lane >> 4) * 8;
-    each<TJ / 2>([&](auto JP) {
-        constexpr int jp = JP.value;
-        const int col = col0 + jp * 32, n = p.cols - col;
-        if (n <= 0) return;
-        const bool whole = p.vectors && n >= 8;
-        float bias[8];
-        if constexpr (EPI != PART && BIN) {
+    // Results: through LDS into rows, so that a lane has eight columns of one row and a few lanes whole lines of memory. The loop over them is a
+    // loop: unrolled over the accumulators, every tile fetched 40 KB of instructions anew (22 - 44 us a tile).
+    constexpr int WJ = BJ / 2, PACKS = WJ / 8, ROWS = (TI < 4 ? TI : 4) * 16, ITEMS = ROWS * PACKS / 64, BATCH = ITEMS < 4 ? ITEMS : 4;
+    unsigned char* const mine = smem + wave * (ROWS * WJ * 4);
+    auto cell = [&](int row, int chunk) { return reinterpret_cast<floatx4*>(mine + row * (WJ * 4) + ((chunk ^ (row & 7)) * 16)); };
+    const int col = j0 + wj * WJ + lane % PACKS * 8, n = p.cols - col;
+    const bool whole = p.vectors && n >= 8;
+    float bias[8];
+    if constexpr (EPI != PART && BIN) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
-            if (p.bias) get8((const uint16_t*)p.bias + col, n >= 8, n, bias);
-        }
-        each<TI>([&](auto I) {
-            constexpr int i = I.value;
-            const int row = row0 + i * 16;
-            if (row >= p.rows) return;
-            float v[8], t[8];
+        for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
+        if (p.bias && n > 0) get8((const uint16_t*)p.bias + col, n >= 8, n, bias);
+    }
+    each<TI * 16 / ROWS>([&](auto H) {
+        constexpr int h = H.value;
+        asm volatile("" ::: "memory");             // (a wavefront's LDS operations are carried out in order)
+        each<ROWS / 16>([&](auto I) {
+            each<TJ>([&](auto J) {
+                *cell(I.value * 16 + (lane & 15), J.value / 2 * 8 + (lane >> 4) * 2 + J.value % 2) = acc[h * (ROWS / 16) + I.value][J.value];
+            });
+        });
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        const int first = i0 + wi * (BI / 2) + h * ROWS;
+#pragma unroll 1
+        for (int it = 0; it < ITEMS; it += BATCH) {
+            float v[BATCH][8], t[BATCH][8], o[BATCH][8];
+            int row[BATCH];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = acc[i][jp * 2 + (e >> 2)][e & 3];
+            for (int u = 0; u < BATCH; ++u) {
+                const int r = (it + u) * (64 / PACKS) + lane / PACKS, c = lane % PACKS * 2;
+                const floatx4 x = *cell(r, c), y = *cell(r, c + 1);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { v[u][e] = x[e]; v[u][4 + e] = y[e]; }
+                row[u] = n > 0 && first + r < p.rows ? first + r : -1;
+            }
             if constexpr (EPI == PART) {
-                put8(p.part + ((int64_t)split * p.rows + row) * p.cols + col, n >= 8 && p.cols % 4 == 0, n, v);
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u)
+                    if (row[u] >= 0) put8(p.part + ((int64_t)split * p.rows + row[u]) * p.cols + col, n >= 8 && p.cols % 4 == 0, n, v[u]);
             } else {
-                if constexpr (BIN) {
+                // what is read from memory, all of it before its use
+                const uint16_t* const other = (const uint16_t*)(BIN ? p.res : p.slope);
+                const int64_t other_ld = BIN ? p.res_ld : p.slope_ld;
+                const bool reads = BIN ? p.res != nullptr : EPI != PURINE_ACT_NONE;
+                if (reads)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += bias[e];
-                    if (p.pre) put8((uint16_t*)p.pre + row * p.pre_ld + col, whole, n, v);
+                    for (int u = 0; u < BATCH; ++u)
+                        if (row[u] >= 0) get8(other + row[u] * other_ld + col, whole, n, t[u]);
+                if (p.accumulate)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = act_of<EPI>(v[e]);
-                    if (p.res) {
-                        get8((const uint16_t*)p.res + row * p.res_ld + col, whole, n, t);
+                    for (int u = 0; u < BATCH; ++u)
+                        if (row[u] >= 0) {
+                            if (p.out_f32) get8((const float*)p.out + row[u] * p.out_ld + col, whole, n, o[u]);
+                            else get8((const uint16_t*)p.out + row[u] * p.out_ld + col, whole, n, o[u]);
+                        }
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += t[e];
+                for (int u = 0; u < BATCH; ++u) {
+                    if (row[u] < 0) continue;
+                    if constexpr (BIN) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[u][e] += bias[e];
+                        if (p.pre) put8((uint16_t*)p.pre + row[u] * p.pre_ld + col, whole, n, v[u]);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[u][e] = act_of<EPI>(v[u][e]);
+                        if (reads)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[u][e] += t[u][e];
+                    } else if constexpr (EPI != PURINE_ACT_NONE) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[u][e] *= act_slope<EPI>(t[u][e]);
                     }
-                } else if constexpr (EPI != PURINE_ACT_NONE) {
-                    get8((const uint16_t*)p.slope + row * p.slope_ld + col, whole, n, t);
+                    if (p.accumulate)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] *= act_slope<EPI>(t[e]);
-                }
-                if (p.out_f32) {
-                    float* o = (float*)p.out + row * p.out_ld + col;
-                    if (p.accumulate) {
-                        get8(o, whole, n, t);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += t[e];
-                    }
-                    put8(o, whole, n, v);
-                } else {
-                    uint16_t* o = (uint16_t*)p.out + row * p.out_ld + col;
-                    if (p.accumulate) {
-                        get8(o, whole, n, t);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += t[e];
-                    }
-                    put8(o, whole, n, v);
+                        for (int e = 0; e < 8; ++e) v[u][e] += o[u][e];
+                    if (p.out_f32) put8((float*)p.out + row[u] * p.out_ld + col, whole, n, v[u]);
+                    else put8((uint16_t*)p.out + row[u] * p.out_ld + col, whole, n, v[u]);
                 }
             }
-        });
+        }
     });
 }
 
