@@ -3,11 +3,16 @@
 //     xhat = (x - mean) rstd,  z = xhat scale[c] + shift[c],  y = act(z)            mean, var: over a group's channels and all positions
 //     dz = dy act'(z),  h = dz scale,  dx = rstd (h - avg(h) - xhat avg(h xhat)),  dshift = sum dz,  dscale = sum dz xhat
 //
-// Bound: HBM. A thread owns V neighbouring channels (16 bytes where the row allows it) and walks down the positions, so that
-// loads are whole rows and the affine parameters stay in registers. Sums are kept per channel, which serves any number of
-// channels per group: for the statistics s = sum (x - k), q = sum (x - k)^2 about the channel's value k at the image's first
-// position (a large mean costs no digits), for the gradient sum dz and sum dz xhat. One kernel sums over slices of the
-// positions, one joins slices and channels in a fixed order, one writes the results.
+// A thread owns V neighbouring channels (16 bytes where the row allows it) and walks down the positions, so that loads are whole pieces of
+// rows and the affine parameters stay in registers. Sums are kept per channel, which serves any number of channels per group: for
+// the statistics s = sum (x - k), q = sum (x - k)^2 about the channel's value k at the image's first position (a large mean
+// costs no digits), for the gradient sum dz and sum dz xhat. They are joined in a fixed order.
+//
+// Bound: HBM, and with an activation the vector units nearly as much (about 30 instructions a gradient element).
+//
+// Where an image's share of a few whole groups fits a workgroup's registers (norm_held_kernel, norm_grad_held_kernel), one workgroup reads it once and
+// writes the results: every tensor moves once. Otherwise (norm_sums / norm_apply) one kernel sums over slices of the positions and a second
+// one joins the slices for itself and reads its tensors again, if they are not too large from the last-level cache.
 #include "activation.h"
 #include "bf16.h"
 #include "block.h"
@@ -17,10 +22,9 @@ namespace {
 
 constexpr int NT = 256;
 
+template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T e[V]; };
 template <typename T, int V>
-__device__ __forceinline__ void load_v(const T* p, float (&v)[V]) {
-    struct alignas(sizeof(T) * V) Pack { T e[V]; };
-    const Pack k = *reinterpret_cast<const Pack*>(p);
+__device__ __forceinline__ void widen_v(const Pack<T, V>& k, float (&v)[V]) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         if constexpr (sizeof(T) == 2) v[i] = bf2f(k.e[i]);
@@ -28,15 +32,41 @@ __device__ __forceinline__ void load_v(const T* p, float (&v)[V]) {
     }
 }
 template <typename T, int V>
+__device__ __forceinline__ void load_v(const T* p, float (&v)[V]) { widen_v<T, V>(*reinterpret_cast<const Pack<T, V>*>(p), v); }
+template <typename T, int V>
 __device__ __forceinline__ void store_v(T* p, const float (&v)[V]) {
-    struct alignas(sizeof(T) * V) Pack { T e[V]; };
-    Pack k;
+    if constexpr (sizeof(T) == 2 && V > 1) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        typedef float floatx2 __attribute__((ext_vector_type(2)));
+        Pack<uint32_t, V / 2> k;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        if constexpr (sizeof(T) == 2) k.e[i] = f2bf(v[i]);
-        else k.e[i] = v[i];
+        for (int i = 0; i < V / 2; ++i) { const floatx2 f = {v[2 * i], v[2 * i + 1]}; k.e[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2)); }
+        *reinterpret_cast<Pack<uint32_t, V / 2>*>(p) = k;
+    } else {
+        Pack<T, V> k;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if constexpr (sizeof(T) == 2) k.e[i] = f2bf(v[i]);
+            else k.e[i] = v[i];
+        }
+        *reinterpret_cast<Pack<T, V>*>(p) = k;
     }
-    *reinterpret_cast<Pack*>(p) = k;
+}
+
+// Makes the compiler forget what it computed from the pieces: it would keep the numbers of one pass over them for the next, in four times the
+// registers.
+template <typename T, int V, int N>
+__device__ __forceinline__ void forget(Pack<T, V> (&k)[N]) {
+    if constexpr (sizeof(T) * V >= 4) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            uint32_t w[sizeof(T) * V / 4];
+            __builtin_memcpy(w, &k[u], sizeof(w));
+#pragma unroll
+            for (unsigned i = 0; i < sizeof(w) / 4; ++i) asm volatile("" : "+v"(w[i]));
+            __builtin_memcpy(&k[u], w, sizeof(w));
+        }
+    }
 }
 
 struct NormParams {
@@ -44,24 +74,54 @@ struct NormParams {
     int64_t x_ns, dy_ns, out_ns;
     const float* scale; const float* shift;     // or null
     float2* part;              // per image, slice and channel: the two sums
-    float2* stat;              // per image and group: mean, rstd; of the gradient avg(h), avg(h xhat)
     const float* mean; const float* rstd;       // gradient: as saved
     float* mean_out; float* rstd_out;           // or null
-    float* dscale; float* dshift;
+    float* dscale; float* dshift;               // or null
     int N, S, C, G, per;       // channels per group
     int slices, rows;          // slices of the positions, positions per slice
     int tiles;                 // of NT vectors of channels
+    int width;                 // held kernels: channels of a workgroup
     float eps;
     int accumulate;
 };
 
-// What a workgroup works on (image, slice of the positions, tile of the channels), the channels of this thread, its place among the
-// threads that share them, and their number.
+// f(group, lane, lanes, sum over the lanes): a few lanes (a power of two) for each of the groups first .. first + count - 1; all threads of
+// the workgroup (THREADS) take part.
+template <int THREADS, typename F>
+__device__ __forceinline__ void for_groups(int count, int per, F&& f) {
+    int lanes = 1;
+    while (lanes < 64 && lanes < per) lanes *= 2;
+    auto sum = [lanes](float v) {
+        for (int d = lanes >> 1; d; d >>= 1) v += __shfl_xor(v, d);
+        return v;
+    };
+    for (int g = threadIdx.x / lanes; g < count; g += THREADS / lanes) f(g, (int)threadIdx.x & (lanes - 1), lanes, sum);
+}
+
+// Mean and rstd of a group from its channels' sums: channel(c, s, q, k) gives those of the group's c-th channel.
+template <typename Sum, typename Channel>
+__device__ __forceinline__ float2 group_stats(const NormParams& p, int lane, int lanes, Sum&& sum, Channel&& channel) {
+    const float n = (float)p.S;
+    float all = 0.0f, s, q, k;
+    for (int c = lane; c < p.per; c += lanes) { channel(c, s, q, k); all += k + s / n; }
+    const float mu = sum(all) / (float)p.per;
+    float var = 0.0f;
+    for (int c = lane; c < p.per; c += lanes) {
+        channel(c, s, q, k);
+        const float d = s / n, off = k + d - mu;
+        var += (fmaxf(q - s * d, 0.0f) + 0.0f * q) / n + off * off;      // (not below zero; infinities stay NaN)
+    }
+    var = sum(var) / (float)p.per;
+    return make_float2(mu, 1.0f / sqrtf(var + p.eps));
+}
+
+// What a workgroup of the kernels over slices works on (image, slice of the positions, tile of the channels), the channels of this thread, its
+// place among the threads that share them, and their number.
 template <int V>
 struct Place {
-    int n, slice, s0, s1, c, r, R, tile;
+    int n, slice, s0, s1, c, r, R, tile, c0, c1;        // c0 .. c1 - 1: the tile's channels
     bool on;
-    __device__ explicit Place(const NormParams& p) {
+    __device__ __forceinline__ explicit Place(const NormParams& p) {
         const int b = blockIdx.x / p.tiles, cv = p.C / V, first = (int)(blockIdx.x - b * p.tiles) * NT;
         n = b / p.slices;
         slice = b - n * p.slices;
@@ -72,6 +132,8 @@ struct Place {
         r = threadIdx.x / tile;
         on = r < R;
         c = (first + (int)threadIdx.x % tile) * V;
+        c0 = first * V;
+        c1 = c0 + tile * V;
     }
 };
 
@@ -93,151 +155,169 @@ __device__ __forceinline__ bool join_rows(const Place<V>& at, float (&s)[V], flo
     return true;
 }
 
+constexpr int AHEAD = 4;                       // positions that a thread loads before it uses the first
+
 template <typename T, int V>
 __global__ __launch_bounds__(NT) void norm_sums_kernel(const NormParams p) {
     const Place<V> at(p);
-    const int n = at.n, s0 = at.s0, s1 = at.s1;
-    const T* x = (const T*)p.x + n * p.x_ns + at.c;
+    const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
     float k[V], s[V], q[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s[i] = q[i] = k[i] = 0.0f;
     if (at.on) {
         load_v<T, V>(x, k);
-        for (int t = s0 + at.r; t < s1; t += at.R) {
-            float v[V];
-            load_v<T, V>(x + (int64_t)t * p.C, v);
+        for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
+            Pack<T, V> in[AHEAD];
 #pragma unroll
-            for (int i = 0; i < V; ++i) { const float d = v[i] - k[i]; s[i] += d; q[i] += d * d; }
+            for (int u = 0; u < AHEAD; ++u) in[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(t + u * at.R, at.s1 - 1) * p.C);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (t + u * at.R >= at.s1) break;
+                float v[V];
+                widen_v<T, V>(in[u], v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) { const float d = v[i] - k[i]; s[i] += d; q[i] += d * d; }
+            }
         }
     }
     if (!join_rows<V>(at, s, q)) return;
-    float2* o = p.part + ((int64_t)n * p.slices + at.slice) * p.C + at.c;
+    float2* o = p.part + ((int64_t)at.n * p.slices + at.slice) * p.C + at.c;
 #pragma unroll
     for (int i = 0; i < V; ++i) o[i] = make_float2(s[i], q[i]);
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+// The sums of a channel over the slices, in order.
+__device__ __forceinline__ float2 over_slices(const NormParams& p, int n, int c) {
+    const float2* part = p.part + (int64_t)n * p.slices * p.C + c;
+    float s = 0.0f, q = 0.0f;
+#pragma unroll 8
+    for (int k = 0; k < p.slices; ++k) { const float2 o = part[(int64_t)k * p.C]; s += o.x; q += o.y; }
+    return make_float2(s, q);
 }
 
-// One wavefront per group: channels' means and squares about them, then the group's.
-template <typename T>
-__global__ __launch_bounds__(64) void norm_stats_kernel(const NormParams p) {
-    const int n = blockIdx.x / p.G, g = blockIdx.x - n * p.G, lane = threadIdx.x;
-    const T* x = (const T*)p.x + n * p.x_ns;
-    const float2* part = p.part + (int64_t)n * p.slices * p.C;
-    auto channel = [&](int c, float& mean, float& m2) {
-        float s = 0.0f, q = 0.0f;
-        for (int k = 0; k < p.slices; ++k) { const float2 o = part[(int64_t)k * p.C + c]; s += o.x; q += o.y; }
-        float v[1];
-        load_v<T, 1>(x + c, v);
-        mean = v[0] + s / (float)p.S;
-        m2 = fmaxf(q - s * (s / (float)p.S), 0.0f) + 0.0f * q;      // (not below zero; infinities stay NaN)
-    };
-    float sum = 0.0f, mean, m2;
-    for (int c = g * p.per + lane; c < (g + 1) * p.per; c += 64) { channel(c, mean, m2); sum += mean; }
-    const float mu = wave_sum(sum) / (float)p.per;
-    float var = 0.0f;
-    for (int c = g * p.per + lane; c < (g + 1) * p.per; c += 64) {
-        channel(c, mean, m2);
-        var += m2 / (float)p.S + (mean - mu) * (mean - mu);
-    }
-    var = wave_sum(var) / (float)p.per;
-    if (lane) return;
-    const float rstd = 1.0f / sqrtf(var + p.eps);
-    p.stat[n * p.G + g] = make_float2(mu, rstd);
-    if (p.mean_out) { p.mean_out[n * p.G + g] = mu; p.rstd_out[n * p.G + g] = rstd; }
-}
-
-// The affine parameters and the group statistics of a thread's channels.
-template <int V>
-struct Affine {
-    float mu[V], rstd[V], scale[V], shift[V];
-    __device__ Affine(const NormParams& p, int n, int c, const float2* stat) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int g = n * p.G + (c + i) / p.per;
-            if (stat) { const float2 o = stat[g]; mu[i] = o.x; rstd[i] = o.y; }
-            else { mu[i] = p.mean[g]; rstd[i] = p.rstd[g]; }
-            scale[i] = p.scale ? p.scale[c + i] : 1.0f;
-            shift[i] = p.shift ? p.shift[c + i] : 0.0f;
-        }
-    }
-};
+// A channel's affine parameters.
+__device__ __forceinline__ float scale_of(const NormParams& p, int c) { return p.scale ? p.scale[c] : 1.0f; }
+__device__ __forceinline__ float shift_of(const NormParams& p, int c) { return p.shift ? p.shift[c] : 0.0f; }
 
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(NT) void norm_apply_kernel(const NormParams p) {
+    __shared__ float2 stat[NT * V + 1];
     const Place<V> at(p);
+    const T* x0 = (const T*)p.x + at.n * p.x_ns;
+    const int g0 = at.c0 / p.per, g1 = (at.c1 - 1) / p.per;
+    for_groups<NT>(g1 - g0 + 1, p.per, [&](int g, int lane, int lanes, auto&& sum) {
+        const int first = (g0 + g) * p.per;
+        const float2 o = group_stats(p, lane, lanes, sum, [&](int c, float& s, float& q, float& k) {
+            const float2 w = over_slices(p, at.n, first + c);
+            float v[1];
+            load_v<T, 1>(x0 + first + c, v);
+            s = w.x; q = w.y; k = v[0];
+        });
+        if (lane == 0) {
+            stat[g] = o;
+            if (at.slice == 0 && p.mean_out) { p.mean_out[at.n * p.G + g0 + g] = o.x; p.rstd_out[at.n * p.G + g0 + g] = o.y; }
+        }
+    });
+    __syncthreads();
     if (!at.on) return;
-    const int n = at.n, s0 = at.s0, s1 = at.s1;
-    const Affine<V> a(p, n, at.c, p.stat);
-    const T* x = (const T*)p.x + n * p.x_ns + at.c;
-    T* y = (T*)p.out + n * p.out_ns + at.c;
-    for (int t = s0 + at.r; t < s1; t += at.R) {
-        float v[V];
-        load_v<T, V>(x + (int64_t)t * p.C, v);
+    float mu[V], a[V], b[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = act_of<ACT>((v[i] - a.mu[i]) * a.rstd[i] * a.scale[i] + a.shift[i]);
-        store_v<T, V>(y + (int64_t)t * p.C, v);
+    for (int i = 0; i < V; ++i) {
+        const float2 o = stat[(at.c + i) / p.per - g0];
+        mu[i] = o.x; a[i] = o.y * scale_of(p, at.c + i); b[i] = shift_of(p, at.c + i);
     }
+    const T* x = x0 + at.c;
+    T* y = (T*)p.out + at.n * p.out_ns + at.c;
+    for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
+        Pack<T, V> in[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) in[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(t + u * at.R, at.s1 - 1) * p.C);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (t + u * at.R >= at.s1) break;
+            float v[V];
+            widen_v<T, V>(in[u], v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = act_of<ACT>((v[i] - mu[i]) * a[i] + b[i]);
+            store_v<T, V>(y + (int64_t)(t + u * at.R) * p.C, v);
+        }
+    }
+}
+
+// x's place in its distribution and the gradient before the activation, of one element.
+template <int ACT>
+__device__ __forceinline__ void grad_of(float x, float dy, float mu, float rstd, float scale, float shift, float& xhat, float& dz) {
+    xhat = (x - mu) * rstd;
+    dz = dy * act_slope<ACT>(xhat * scale + shift);
 }
 
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(NT) void norm_grad_sums_kernel(const NormParams p) {
     const Place<V> at(p);
-    const int n = at.n, s0 = at.s0, s1 = at.s1;
     float s[V], q[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s[i] = q[i] = 0.0f;
     if (at.on) {
-        const Affine<V> a(p, n, at.c, nullptr);
-        const T* x = (const T*)p.x + n * p.x_ns + at.c;
-        const T* dy = (const T*)p.dy + n * p.dy_ns + at.c;
-        for (int t = s0 + at.r; t < s1; t += at.R) {
-            float v[V], d[V];
-            load_v<T, V>(x + (int64_t)t * p.C, v);
-            load_v<T, V>(dy + (int64_t)t * p.C, d);
+        float mu[V], rstd[V], sc[V], sh[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float xhat = (v[i] - a.mu[i]) * a.rstd[i], dz = d[i] * act_slope<ACT>(xhat * a.scale[i] + a.shift[i]);
-                s[i] += dz;
-                q[i] += dz * xhat;
+        for (int i = 0; i < V; ++i) {
+            const int g = at.n * p.G + (at.c + i) / p.per;
+            mu[i] = p.mean[g]; rstd[i] = p.rstd[g]; sc[i] = scale_of(p, at.c + i); sh[i] = shift_of(p, at.c + i);
+        }
+        const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
+        const T* dy = (const T*)p.dy + at.n * p.dy_ns + at.c;
+        for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
+            Pack<T, V> in[AHEAD], gr[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t row = (int64_t)min(t + u * at.R, at.s1 - 1) * p.C;
+                in[u] = *reinterpret_cast<const Pack<T, V>*>(x + row);
+                gr[u] = *reinterpret_cast<const Pack<T, V>*>(dy + row);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (t + u * at.R >= at.s1) break;
+                float v[V], d[V];
+                widen_v<T, V>(in[u], v);
+                widen_v<T, V>(gr[u], d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float xhat, dz;
+                    grad_of<ACT>(v[i], d[i], mu[i], rstd[i], sc[i], sh[i], xhat, dz);
+                    s[i] += dz;
+                    q[i] += dz * xhat;
+                }
             }
         }
     }
     if (!join_rows<V>(at, s, q)) return;
-    float2* o = p.part + ((int64_t)n * p.slices + at.slice) * p.C + at.c;
+    float2* o = p.part + ((int64_t)at.n * p.slices + at.slice) * p.C + at.c;
 #pragma unroll
     for (int i = 0; i < V; ++i) o[i] = make_float2(s[i], q[i]);
 }
 
-__global__ __launch_bounds__(64) void norm_grad_stats_kernel(const NormParams p) {
-    const int n = blockIdx.x / p.G, g = blockIdx.x - n * p.G, lane = threadIdx.x;
-    const float2* part = p.part + (int64_t)n * p.slices * p.C;
+// avg(h), avg(h xhat) of a group from its channels' sums.
+template <typename Sum, typename Channel>
+__device__ __forceinline__ float2 group_averages(const NormParams& p, int lane, int lanes, Sum&& sum, Channel&& channel) {
     float a = 0.0f, b = 0.0f;
-    for (int c = g * p.per + lane; c < (g + 1) * p.per; c += 64) {
-        float s = 0.0f, q = 0.0f;
-        for (int k = 0; k < p.slices; ++k) { const float2 o = part[(int64_t)k * p.C + c]; s += o.x; q += o.y; }
-        const float w = p.scale ? p.scale[c] : 1.0f;
-        a += s * w;
-        b += q * w;
+    for (int c = lane; c < p.per; c += lanes) {
+        float w;
+        const float2 o = channel(c, w);
+        a += o.x * w;
+        b += o.y * w;
     }
-    a = wave_sum(a);
-    b = wave_sum(b);
     const float count = (float)p.per * (float)p.S;
-    if (lane == 0) p.stat[n * p.G + g] = make_float2(a / count, b / count);
+    return make_float2(sum(a) / count, sum(b) / count);
 }
 
-// dscale, dshift: a wavefront per 64 channels' worth of sums would leave the chip idle; 256 threads per 16 channels share the
-// images and slices, and join in LDS.
-__global__ __launch_bounds__(NT) void norm_grad_params_kernel(const NormParams p) {
+// dscale and dshift of 16 channels: 16 threads each share the images and slices, and join in LDS.
+__device__ __forceinline__ void param_sums(const NormParams& p, int first) {
     __shared__ float2 sums[16][17];
-    const int l = threadIdx.x & 15, r = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
+    const int l = threadIdx.x & 15, r = threadIdx.x >> 4, c = first + l;
     const int64_t rows = (int64_t)p.N * p.slices;
     float s = 0.0f, q = 0.0f;
     if (c < p.C)
+#pragma unroll 8
         for (int64_t k = r; k < rows; k += 16) { const float2 o = p.part[k * p.C + c]; s += o.x; q += o.y; }
     sums[r][l] = make_float2(s, q);
     __syncthreads();
@@ -246,31 +326,220 @@ __global__ __launch_bounds__(NT) void norm_grad_params_kernel(const NormParams p
     p.dshift[c] = s;
     p.dscale[c] = q;
 }
+__global__ __launch_bounds__(NT) void norm_grad_params_kernel(const NormParams p) { param_sums(p, blockIdx.x * 16); }
 
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(NT) void norm_grad_apply_kernel(const NormParams p) {
+    __shared__ float2 stat[NT * V + 1];
     const Place<V> at(p);
+    const int g0 = at.c0 / p.per, g1 = (at.c1 - 1) / p.per;
+    for_groups<NT>(g1 - g0 + 1, p.per, [&](int g, int lane, int lanes, auto&& sum) {
+        const int first = (g0 + g) * p.per;
+        const float2 o = group_averages(p, lane, lanes, sum, [&](int c, float& w) { w = scale_of(p, first + c); return over_slices(p, at.n, first + c); });
+        if (lane == 0) stat[g] = o;
+    });
+    __syncthreads();
     if (!at.on) return;
-    const int n = at.n, s0 = at.s0, s1 = at.s1;
-    const Affine<V> a(p, n, at.c, nullptr);
-    float ah[V], ahx[V];
+    float mu[V], rstd[V], sc[V], sh[V], c1[V], c2[V], rs[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) { const float2 o = p.stat[n * p.G + (at.c + i) / p.per]; ah[i] = o.x; ahx[i] = o.y; }
-    const T* x = (const T*)p.x + n * p.x_ns + at.c;
-    const T* dy = (const T*)p.dy + n * p.dy_ns + at.c;
-    T* dx = (T*)p.out + n * p.out_ns + at.c;
-    for (int t = s0 + at.r; t < s1; t += at.R) {
-        float v[V], d[V], old[V];
-        load_v<T, V>(x + (int64_t)t * p.C, v);
-        load_v<T, V>(dy + (int64_t)t * p.C, d);
-        if (p.accumulate) load_v<T, V>(dx + (int64_t)t * p.C, old);
+    for (int i = 0; i < V; ++i) {
+        const int gi = (at.c + i) / p.per, g = at.n * p.G + gi;
+        const float2 o = stat[gi - g0];
+        mu[i] = p.mean[g]; rstd[i] = p.rstd[g]; sc[i] = scale_of(p, at.c + i); sh[i] = shift_of(p, at.c + i);
+        c1[i] = rstd[i] * o.x; c2[i] = rstd[i] * o.y; rs[i] = rstd[i] * sc[i];
+    }
+    const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
+    const T* dy = (const T*)p.dy + at.n * p.dy_ns + at.c;
+    T* dx = (T*)p.out + at.n * p.out_ns + at.c;
+    for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
+        Pack<T, V> in[AHEAD], gr[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t row = (int64_t)min(t + u * at.R, at.s1 - 1) * p.C;
+            in[u] = *reinterpret_cast<const Pack<T, V>*>(x + row);
+            gr[u] = *reinterpret_cast<const Pack<T, V>*>(dy + row);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (t + u * at.R >= at.s1) break;
+            T* o = dx + (int64_t)(t + u * at.R) * p.C;
+            float v[V], d[V], old[V];
+            widen_v<T, V>(in[u], v);
+            widen_v<T, V>(gr[u], d);
+            if (p.accumulate) load_v<T, V>(o, old);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float xhat, dz;
+                grad_of<ACT>(v[i], d[i], mu[i], rstd[i], sc[i], sh[i], xhat, dz);
+                v[i] = dz * rs[i] - (xhat * c2[i] + c1[i]);
+                if (p.accumulate) v[i] += old[i];
+            }
+            store_v<T, V>(o, v);
+        }
+    }
+}
+
+// ---- an image's share of a few whole groups, in registers
+constexpr int HT = 512, HELD = 16, HELD_GRAD = 10;      // threads; pieces of a thread at most, and of eight bf16 numbers in the gradient (120 registers)
+
+// Consecutive workgroups go to the eight dies in turn; those of one image share lines of memory, so a die takes consecutive ones.
+__device__ __forceinline__ int held_block() {
+    const int total = gridDim.x, per = total >> 3, b = blockIdx.x;
+    return per > 0 && b < per * 8 ? (b & 7) * per + (b >> 3) : b;
+}
+// Sums of every channel of the workgroup, from each thread's: left in `chan` (width of them).
+template <int V, int THREADS>
+__device__ __forceinline__ void join_held(const float (&s)[V], const float (&q)[V], float2* sums, float2* chan, int width, int R, bool on) {
+    if (on)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sums[threadIdx.x * V + i] = make_float2(s[i], q[i]);        // [r][channel]
+    __syncthreads();
+    // width channels over THREADS / width threads each, then over one
+    const int lanes = THREADS / width, c = threadIdx.x % width, l = threadIdx.x / width;
+    float2 t = make_float2(0.0f, 0.0f);
+    if (l < lanes)
+        for (int r = l; r < R; r += lanes) { const float2 o = sums[r * width + c]; t.x += o.x; t.y += o.y; }
+    __syncthreads();
+    if (l < lanes) sums[l * width + c] = t;
+    __syncthreads();
+    if (threadIdx.x < width) {
+        for (int k = 1; k < min(lanes, R); ++k) { const float2 o = sums[k * width + c]; t.x += o.x; t.y += o.y; }
+        chan[c] = t;
+    }
+    __syncthreads();
+}
+
+template <typename T, int V, int ACT, int NV, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_held_kernel(const NormParams p) {
+    __shared__ float2 sums[THREADS * V], chan[THREADS], stat[THREADS];
+    const int b = held_block(), n = b / p.tiles, c0 = (b - n * p.tiles) * p.width, cv = p.width / V, R = THREADS / cv;
+    const int r = threadIdx.x / cv, c = c0 + (int)threadIdx.x % cv * V;
+    const bool on = r < R;
+    const T* x0 = (const T*)p.x + n * p.x_ns;
+    const T* x = x0 + c;
+    Pack<T, V> in[NV];
+    float k[V], s[V], q[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] = q[i] = k[i] = 0.0f;
+    if (on) {
+        load_v<T, V>(x, k);
+#pragma unroll
+        for (int u = 0; u < NV; ++u) in[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(r + u * R, p.S - 1) * p.C);
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            if (r + u * R >= p.S) break;
+            float v[V];
+            widen_v<T, V>(in[u], v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) { const float d = v[i] - k[i]; s[i] += d; q[i] += d * d; }
+        }
+    }
+    join_held<V, THREADS>(s, q, sums, chan, p.width, R, on);
+    for_groups<THREADS>(p.width / p.per, p.per, [&](int g, int lane, int lanes, auto&& sum) {
+        const float2 o = group_stats(p, lane, lanes, sum, [&](int i, float& cs, float& cq, float& ck) {
+            const float2 w = chan[g * p.per + i];
+            float v[1];
+            load_v<T, 1>(x0 + c0 + g * p.per + i, v);
+            cs = w.x; cq = w.y; ck = v[0];
+        });
+        if (lane == 0) {
+            stat[g] = o;
+            const int at = n * p.G + c0 / p.per + g;
+            if (p.mean_out) { p.mean_out[at] = o.x; p.rstd_out[at] = o.y; }
+        }
+    });
+    __syncthreads();
+    if (!on) return;
+    float mu[V], a[V], sh[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float2 o = stat[(c + i - c0) / p.per];
+        mu[i] = o.x; a[i] = o.y * scale_of(p, c + i); sh[i] = shift_of(p, c + i);
+    }
+    T* y = (T*)p.out + n * p.out_ns + c;
+    forget(in);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+        if (r + u * R >= p.S) break;
+        float v[V];
+        widen_v<T, V>(in[u], v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = act_of<ACT>((v[i] - mu[i]) * a[i] + sh[i]);
+        store_v<T, V>(y + (int64_t)(r + u * R) * p.C, v);
+    }
+}
+
+// (dz stays in fp32 between the passes: with x and dy held and the slope computed again, 128 x 784 x 192 in bf16 took 46 us)
+template <typename T, int V, int ACT, int NV, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_grad_held_kernel(const NormParams p) {
+    __shared__ float2 sums[THREADS * V], chan[THREADS], stat[THREADS];
+    const int b = held_block(), n = b / p.tiles, c0 = (b - n * p.tiles) * p.width, cv = p.width / V, R = THREADS / cv;
+    const int r = threadIdx.x / cv, c = c0 + (int)threadIdx.x % cv * V;
+    const bool on = r < R;
+    const T* x = (const T*)p.x + n * p.x_ns + c;
+    const T* dy = (const T*)p.dy + n * p.dy_ns + c;
+    Pack<T, V> in[NV];
+    float dz[NV][V], mu[V], rstd[V], s[V], q[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] = q[i] = mu[i] = rstd[i] = 0.0f;
+    if (on) {
+        Pack<T, V> gr[NV];
+        float sc[V], sh[V];
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            const int64_t row = (int64_t)min(r + u * R, p.S - 1) * p.C;
+            in[u] = *reinterpret_cast<const Pack<T, V>*>(x + row);
+            gr[u] = *reinterpret_cast<const Pack<T, V>*>(dy + row);
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float xhat = (v[i] - a.mu[i]) * a.rstd[i], h = d[i] * act_slope<ACT>(xhat * a.scale[i] + a.shift[i]) * a.scale[i];
-            v[i] = a.rstd[i] * (h - ah[i] - xhat * ahx[i]);
+            const int g = n * p.G + (c + i) / p.per;
+            mu[i] = p.mean[g]; rstd[i] = p.rstd[g]; sc[i] = scale_of(p, c + i); sh[i] = shift_of(p, c + i);
+        }
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            if (r + u * R >= p.S) break;
+            float v[V], d[V];
+            widen_v<T, V>(in[u], v);
+            widen_v<T, V>(gr[u], d);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float xhat;
+                grad_of<ACT>(v[i], d[i], mu[i], rstd[i], sc[i], sh[i], xhat, dz[u][i]);
+                s[i] += dz[u][i];
+                q[i] += dz[u][i] * xhat;
+            }
+        }
+    }
+    join_held<V, THREADS>(s, q, sums, chan, p.width, R, on);
+    if (p.dscale && threadIdx.x < p.width) p.part[(int64_t)n * p.C + c0 + threadIdx.x] = chan[threadIdx.x];
+    for_groups<THREADS>(p.width / p.per, p.per, [&](int g, int lane, int lanes, auto&& sum) {
+        const float2 o = group_averages(p, lane, lanes, sum, [&](int i, float& w) { w = scale_of(p, c0 + g * p.per + i); return chan[g * p.per + i]; });
+        if (lane == 0) stat[g] = o;
+    });
+    __syncthreads();
+    if (!on) return;
+    float c1[V], c2[V], rs[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float2 o = stat[(c + i - c0) / p.per];
+        c1[i] = rstd[i] * o.x; c2[i] = rstd[i] * o.y; rs[i] = rstd[i] * scale_of(p, c + i);
+    }
+    T* dx = (T*)p.out + n * p.out_ns + c;
+    forget(in);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+        if (r + u * R >= p.S) break;
+        T* o = dx + (int64_t)(r + u * R) * p.C;
+        float v[V], old[V];
+        widen_v<T, V>(in[u], v);
+        if (p.accumulate) load_v<T, V>(o, old);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            v[i] = dz[u][i] * rs[i] - ((v[i] - mu[i]) * rstd[i] * c2[i] + c1[i]);
             if (p.accumulate) v[i] += old[i];
         }
-        store_v<T, V>(dx + (int64_t)t * p.C, v);
+        store_v<T, V>(o, v);
     }
 }
 
@@ -286,6 +555,29 @@ int vector_of(int64_t C, int dtype) {
     for (int v = dtype == PURINE_BF16 ? 8 : 4; v > 1; v >>= 1)
         if (C % v == 0) return v;
     return 1;
+}
+
+// Channels of a workgroup that holds its share of an image in registers, and its pieces per thread; 0 where that does not apply. Whole
+// groups and whole pieces; as wide as fits up to a line of memory (128 bytes), unless that leaves fewer than 512 workgroups.
+struct HeldPlan { int width, pieces, threads; };
+HeldPlan held_plan(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, int v, bool backward) {
+    const int64_t per = C / G, bytes = dtype == PURINE_BF16 ? 2 : 4;
+    int64_t unit = per;
+    while (unit % v) unit += per;
+    HeldPlan best{0, 0, 0};
+    if (unit > C || C % unit) return best;
+    for (int64_t m = 1; unit * m <= C; ++m) {
+        const int64_t w = unit * m, cv = w / v;
+        if (C % w) continue;
+        if (w > 256 || cv > 256) break;
+        if (best.width && (w * bytes > 128 && best.width * bytes >= 64)) break;
+        if (best.width && N * (C / w) < 512) break;
+        const int threads = S * cv <= 256 * 4 ? 256 : HT;
+        const int64_t R = threads / cv, pieces = (S + R - 1) / R;
+        if (pieces > (backward && v == 8 ? HELD_GRAD : HELD)) break;
+        best = HeldPlan{(int)w, (int)pieces, threads};
+    }
+    return best;
 }
 
 template <typename F>
@@ -315,6 +607,15 @@ hipError_t by_vector(int dtype, int v, F&& f) {
         default: return f(float(), std::integral_constant<int, 1>());
     }
 }
+// f(pieces as a constant, threads as a constant)
+template <int MOST, typename F>
+hipError_t by_pieces(const HeldPlan& h, F&& f) {
+    if (h.threads == 256) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 256>());
+    if (h.pieces <= 4) return f(std::integral_constant<int, 4>(), std::integral_constant<int, HT>());
+    if (h.pieces <= HELD_GRAD) return f(std::integral_constant<int, HELD_GRAD>(), std::integral_constant<int, HT>());
+    if constexpr (MOST > HELD_GRAD) return f(std::integral_constant<int, MOST>(), std::integral_constant<int, HT>());
+    return hipErrorInvalidValue;
+}
 
 NormParams params_of(const NormShape& s, void* ws) {
     NormParams p{};
@@ -324,8 +625,7 @@ NormParams params_of(const NormShape& s, void* ws) {
     p.slices = slices_of(s.N, s.S, s.C);
     p.rows = (s.S + p.slices - 1) / p.slices;
     p.slices = (s.S + p.rows - 1) / p.rows;
-    p.stat = (float2*)ws;
-    p.part = p.stat + (size_t)s.N * s.G;
+    p.part = (float2*)ws;
     return p;
 }
 
@@ -334,12 +634,18 @@ unsigned grid_of(NormParams& p, int v) {
     p.tiles = (p.C / v + NT - 1) / NT;
     return (unsigned)((int64_t)p.N * p.slices * p.tiles);
 }
+unsigned held_grid(NormParams& p, const HeldPlan& h) {
+    p.width = h.width;
+    p.tiles = p.C / h.width;
+    p.slices = 1;
+    return (unsigned)((int64_t)p.N * p.tiles);
+}
 
 }  // namespace
 
-size_t group_norm_ws_bytes(bool, int64_t N, int64_t S, int64_t C, int64_t G, int) {
-    const int64_t slices = slices_of(N, S, C);
-    return (size_t)(N * G + N * slices * C) * sizeof(float2);
+size_t group_norm_ws_bytes(bool backward, int64_t N, int64_t S, int64_t C, int64_t G, int dtype) {
+    const bool held = held_plan(N, S, C, G, dtype, vector_of(C, dtype), backward).width != 0;
+    return held ? (backward ? (size_t)(N * C) * sizeof(float2) : 0) : (size_t)(N * slices_of(N, S, C) * C) * sizeof(float2);
 }
 
 hipError_t launch_group_norm_fwd(int dtype, const NormShape& s, const void* x, const float* scale, const float* shift, void* y, float* mean,
@@ -348,13 +654,21 @@ hipError_t launch_group_norm_fwd(int dtype, const NormShape& s, const void* x, c
     p.x = x; p.scale = scale; p.shift = shift; p.out = y; p.out_ns = s.y_ns;
     p.mean_out = mean; p.rstd_out = rstd;
     const int v = vector_of(s.C, dtype);
-    const unsigned grid = grid_of(p, v);
+    const HeldPlan h = held_plan(s.N, s.S, s.C, s.G, dtype, v, false);
     (void)hipGetLastError();
     return by_vector(dtype, v, [&](auto t, auto V) {
         typedef decltype(t) T;
-        hipLaunchKernelGGL((norm_sums_kernel<T, V.value>), dim3(grid), dim3(NT), 0, st, p);
-        hipLaunchKernelGGL((norm_stats_kernel<T>), dim3(p.N * p.G), dim3(64), 0, st, p);
         return by_act(s.act, [&](auto A) {
+            if (h.width) {
+                const unsigned grid = held_grid(p, h);
+                ProbeScope probe(st);
+                return by_pieces<HELD>(h, [&](auto P, auto H) {
+                    hipLaunchKernelGGL((norm_held_kernel<T, V.value, A.value, P.value, H.value>), dim3(grid), dim3(H.value), 0, st, p);
+                    return hipGetLastError();
+                });
+            }
+            const unsigned grid = grid_of(p, v);
+            hipLaunchKernelGGL((norm_sums_kernel<T, V.value>), dim3(grid), dim3(NT), 0, st, p);
             ProbeScope probe(st);
             hipLaunchKernelGGL((norm_apply_kernel<T, V.value, A.value>), dim3(grid), dim3(NT), 0, st, p);
             return hipGetLastError();
@@ -369,19 +683,29 @@ hipError_t launch_group_norm_bwd(int dtype, const NormShape& s, const void* x, c
     p.out = dx; p.out_ns = s.dx_ns; p.dscale = dscale; p.dshift = dshift;
     p.accumulate = beta != 0.0f;
     const int v = vector_of(s.C, dtype);
-    const unsigned grid = grid_of(p, v);
+    const HeldPlan h = held_plan(s.N, s.S, s.C, s.G, dtype, v, true);
     (void)hipGetLastError();
-    return by_vector(dtype, v, [&](auto t, auto V) {
+    const hipError_t e = by_vector(dtype, v, [&](auto t, auto V) {
         typedef decltype(t) T;
         return by_act(s.act, [&](auto A) {
+            if (h.width) {
+                const unsigned grid = held_grid(p, h);
+                ProbeScope probe(st);
+                return by_pieces<V.value == 8 ? HELD_GRAD : HELD>(h, [&](auto P, auto H) {
+                    hipLaunchKernelGGL((norm_grad_held_kernel<T, V.value, A.value, P.value, H.value>), dim3(grid), dim3(H.value), 0, st, p);
+                    return hipGetLastError();
+                });
+            }
+            const unsigned grid = grid_of(p, v);
             hipLaunchKernelGGL((norm_grad_sums_kernel<T, V.value, A.value>), dim3(grid), dim3(NT), 0, st, p);
-            hipLaunchKernelGGL(norm_grad_stats_kernel, dim3(p.N * p.G), dim3(64), 0, st, p);
-            if (dscale) hipLaunchKernelGGL(norm_grad_params_kernel, dim3((p.C + 15) / 16), dim3(NT), 0, st, p);
             ProbeScope probe(st);
             hipLaunchKernelGGL((norm_grad_apply_kernel<T, V.value, A.value>), dim3(grid), dim3(NT), 0, st, p);
             return hipGetLastError();
         });
     });
+    if (e != hipSuccess || !dscale) return e;
+    hipLaunchKernelGGL(norm_grad_params_kernel, dim3((p.C + 15) / 16), dim3(NT), 0, st, p);
+    return hipGetLastError();
 }
 
 }  // namespace purine
