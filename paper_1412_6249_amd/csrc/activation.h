@@ -16,7 +16,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float inverse_of_1_plus_pow2(float u) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u)); }
 __device__ __forceinline__ float sigmoid(float z) { return inverse_of_1_plus_pow2(-kLog2e * z); }
 // 0.5 (1 + tanh u) = sigmoid(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3)
-__device__ __forceinline__ float tanh_gate(float z) { return inverse_of_1_plus_pow2(z * (-2.0f * kLog2e * kTanhIn - 2.0f * kLog2e * kTanhIn * kTanhCube * z * z)); }
+constexpr float kGate1 = -2.0f * kLog2e * kTanhIn, kGate3 = kGate1 * kTanhCube;
+__device__ __forceinline__ float tanh_gate(float z) { return inverse_of_1_plus_pow2(z * (kGate1 + kGate3 * (z * z))); }
 
 // The normal distribution's integral up to z, and exp(-z^2 / 2). Abramowitz and Stegun 7.1.26: erfc(x) = P(t) exp(-x^2) with
 // t = 1 / (1 + 0.3275911 x), off by 1.5e-7 at most.
@@ -48,7 +49,7 @@ __device__ __forceinline__ float act_slope(float z) {
     const float c = __builtin_amdgcn_fmed3f(z, -100.0f, 100.0f);
     if constexpr (ACT == PURINE_ACT_SILU) {
         const float s = sigmoid(z);
-        return s * (1.0f + c * (1.0f - s));
+        return s + (c - c * s) * s;
     }
     if constexpr (ACT == PURINE_ACT_GELU) {
         float e;
@@ -56,8 +57,8 @@ __device__ __forceinline__ float act_slope(float z) {
         return n + c * (e * 0.3989422804014327f);
     }
     if constexpr (ACT == PURINE_ACT_GELU_TANH) {
-        const float s = tanh_gate(z);
-        return s * (1.0f + c * (1.0f - s) * (2.0f * kTanhIn + 6.0f * kTanhIn * kTanhCube * c * c));
+        const float u = c * c, s = inverse_of_1_plus_pow2(z * (kGate1 + kGate3 * u));
+        return s + s * ((c - c * s) * (2.0f * kTanhIn + 6.0f * kTanhIn * kTanhCube * u));
     }
     return 1.0f;
 }
