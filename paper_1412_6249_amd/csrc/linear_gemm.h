@@ -229,12 +229,14 @@ __device__ __forceinline__ void settle(floatx4 (&c)[TI][TJ]) {
     else asm volatile("s_nop 15\n\ts_nop 15" : LIN_C2(c, I));
 }
 
+__device__ __forceinline__ void widen8(const u32x4& k, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(k[e] << 16); v[2 * e + 1] = __uint_as_float(k[e] & 0xffff0000u); }
+}
 // Eight values of a row, from and to memory: whole (16-byte aligned), or those of the first `n`.
 __device__ __forceinline__ void get8(const uint16_t* p, bool whole, int n, float (&v)[8]) {
     if (whole) {
-        const u32x4 k = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(k[e] << 16); v[2 * e + 1] = __uint_as_float(k[e] & 0xffff0000u); }
+        widen8(*reinterpret_cast<const u32x4*>(p), v);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = e < n ? bf2f(p[e]) : 0.0f;
@@ -424,13 +426,29 @@ __global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear
     unsigned char* const mine = smem + wave * (ROWS * WJ * 4);
     auto cell = [&](int row, int chunk) { return reinterpret_cast<floatx4*>(mine + row * (WJ * 4) + ((chunk ^ (row & 7)) * 16)); };
     const int col = j0 + wj * WJ + lane % PACKS * 8, n = p.cols - col;
-    const bool whole = p.vectors && n >= 8;
+    const bool inside = p.vectors && j0 + BJ <= p.cols;        // every lane's eight columns exist and are 16 bytes
     float bias[8];
     if constexpr (EPI != PART && BIN) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
         if (p.bias && n > 0) get8((const uint16_t*)p.bias + col, n >= 8, n, bias);
     }
+    // what is read from memory besides the sums: the residual, or what the slope is taken of
+    const uint16_t* const other = (const uint16_t*)(BIN ? p.res : p.slope);
+    const int64_t other_ld = BIN ? p.res_ld : p.slope_ld;
+    const bool reads = EPI != PART && (BIN ? p.res != nullptr : EPI != PURINE_ACT_NONE);
+    auto combine = [&](float (&v)[8], const float (&t)[8], float (&pre)[8]) {
+        if constexpr (EPI != PART && BIN) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { pre[e] = v[e] + bias[e]; v[e] = act_of<EPI>(pre[e]); }
+            if (reads)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += t[e];
+        } else if constexpr (EPI != PART && EPI != PURINE_ACT_NONE) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= act_slope<EPI>(t[e]);
+        }
+    };
     each<TI * 16 / ROWS>([&](auto H) {
         constexpr int h = H.value;
         asm volatile("" ::: "memory");             // (a wavefront's LDS operations are carried out in order)
@@ -442,59 +460,67 @@ __global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear
         asm volatile("" ::: "memory");
         __builtin_amdgcn_wave_barrier();
         const int first = i0 + wi * (BI / 2) + h * ROWS;
+        auto item = [&](int k, float (&v)[8]) {
+            const int r = k * (64 / PACKS) + lane / PACKS, c = lane % PACKS * 2;
+            const floatx4 x = *cell(r, c), y = *cell(r, c + 1);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] = x[e]; v[4 + e] = y[e]; }
+            return first + r;
+        };
+        if (EPI != PART && inside && !p.out_f32) {
+            // everything that is read is asked for before any of it is used, without a branch between (rows past the last read it)
 #pragma unroll 1
-        for (int it = 0; it < ITEMS; it += BATCH) {
-            float v[BATCH][8], t[BATCH][8], o[BATCH][8];
-            int row[BATCH];
+            for (int it = 0; it < ITEMS; it += BATCH) {
+                float v[BATCH][8];
+                u32x4 t[BATCH], o[BATCH];
+                int row[BATCH];
 #pragma unroll
-            for (int u = 0; u < BATCH; ++u) {
-                const int r = (it + u) * (64 / PACKS) + lane / PACKS, c = lane % PACKS * 2;
-                const floatx4 x = *cell(r, c), y = *cell(r, c + 1);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { v[u][e] = x[e]; v[u][4 + e] = y[e]; }
-                row[u] = n > 0 && first + r < p.rows ? first + r : -1;
-            }
-            if constexpr (EPI == PART) {
-#pragma unroll
-                for (int u = 0; u < BATCH; ++u)
-                    if (row[u] >= 0) put8(p.part + ((int64_t)split * p.rows + row[u]) * p.cols + col, n >= 8 && p.cols % 4 == 0, n, v[u]);
-            } else {
-                // what is read from memory, all of it before its use
-                const uint16_t* const other = (const uint16_t*)(BIN ? p.res : p.slope);
-                const int64_t other_ld = BIN ? p.res_ld : p.slope_ld;
-                const bool reads = BIN ? p.res != nullptr : EPI != PURINE_ACT_NONE;
+                for (int u = 0; u < BATCH; ++u) row[u] = first + (it + u) * (64 / PACKS) + lane / PACKS;
                 if (reads)
 #pragma unroll
-                    for (int u = 0; u < BATCH; ++u)
-                        if (row[u] >= 0) get8(other + row[u] * other_ld + col, whole, n, t[u]);
+                    for (int u = 0; u < BATCH; ++u) t[u] = *reinterpret_cast<const u32x4*>(other + min(row[u], p.rows - 1) * other_ld + col);
                 if (p.accumulate)
 #pragma unroll
-                    for (int u = 0; u < BATCH; ++u)
-                        if (row[u] >= 0) {
-                            if (p.out_f32) get8((const float*)p.out + row[u] * p.out_ld + col, whole, n, o[u]);
-                            else get8((const uint16_t*)p.out + row[u] * p.out_ld + col, whole, n, o[u]);
-                        }
+                    for (int u = 0; u < BATCH; ++u) o[u] = *reinterpret_cast<const u32x4*>((const uint16_t*)p.out + min(row[u], p.rows - 1) * p.out_ld + col);
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) item(it + u, v[u]);
 #pragma unroll
                 for (int u = 0; u < BATCH; ++u) {
-                    if (row[u] < 0) continue;
-                    if constexpr (BIN) {
+                    float w[8], pre[8];
+                    if (reads) widen8(t[u], w);
+                    combine(v[u], w, pre);
+                    if (p.accumulate) {
+                        widen8(o[u], w);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[u][e] += bias[e];
-                        if (p.pre) put8((uint16_t*)p.pre + row[u] * p.pre_ld + col, whole, n, v[u]);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[u][e] = act_of<EPI>(v[u][e]);
-                        if (reads)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[u][e] += t[u][e];
-                    } else if constexpr (EPI != PURINE_ACT_NONE) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[u][e] *= act_slope<EPI>(t[u][e]);
+                        for (int e = 0; e < 8; ++e) v[u][e] += w[e];
                     }
-                    if (p.accumulate)
+                    if (row[u] < p.rows) {
+                        if (BIN && p.pre) put8((uint16_t*)p.pre + row[u] * p.pre_ld + col, true, 8, pre);
+                        put8((uint16_t*)p.out + row[u] * p.out_ld + col, true, 8, v[u]);
+                    }
+                }
+            }
+        } else {
+            const bool whole = n >= 8 && (EPI == PART ? p.cols % 4 == 0 : p.vectors);
+#pragma unroll 1
+            for (int it = 0; it < ITEMS; ++it) {
+                float v[8], t[8], pre[8];
+                const int row = item(it, v);
+                if (row >= p.rows || n <= 0) continue;
+                if constexpr (EPI == PART) {
+                    put8(p.part + ((int64_t)split * p.rows + row) * p.cols + col, whole, n, v);
+                } else {
+                    if (reads) get8(other + row * other_ld + col, whole, n, t);
+                    combine(v, t, pre);
+                    if (BIN && p.pre) put8((uint16_t*)p.pre + row * p.pre_ld + col, whole, n, pre);
+                    if (p.accumulate) {
+                        if (p.out_f32) get8((const float*)p.out + row * p.out_ld + col, whole, n, t);
+                        else get8((const uint16_t*)p.out + row * p.out_ld + col, whole, n, t);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[u][e] += o[u][e];
-                    if (p.out_f32) put8((float*)p.out + row[u] * p.out_ld + col, whole, n, v[u]);
-                    else put8((uint16_t*)p.out + row[u] * p.out_ld + col, whole, n, v[u]);
+                        for (int e = 0; e < 8; ++e) v[e] += t[e];
+                    }
+                    if (p.out_f32) put8((float*)p.out + row * p.out_ld + col, whole, n, v);
+                    else put8((uint16_t*)p.out + row * p.out_ld + col, whole, n, v);
                 }
             }
         }
