@@ -142,35 +142,37 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const JoinParams p) {
 
 // How a product is computed: the same answer for the workspace query and for the launch.
 struct GemmPlan {
-    int tile, tiles_i, tiles_j, steps, splits, per_split;
+    int tile, bufs, tiles_i, tiles_j, steps, splits, per_split;
     double us;
 };
 
-// Tiles of 256, 128 or 64 on a side, the reduction split where tiles alone leave compute units idle: the least expected time. A step of 64 takes a
-// compute unit `step` cycles per tile once enough tiles are there to overlap; alone on it a tile takes `alone`.
-struct TileCost { int tile, resident; double step, alone; };
-constexpr TileCost kTiles[] = {{256, 1, 2400, 2400}, {128, 2, 800, 1100}, {64, 4, 330, 800}};
+// The forms of the kernel on the matrix cores, and what a compute unit takes with them (us, measured at 1024 and 8192 on a side over 64 to 4096):
+// workgroups that it holds; a round of them apart from its steps (first loads, results); a step of 64 with all of them, and with one.
+struct Form { int tile, bufs, resident; double round, step, alone; };
+constexpr Form kForms[] = {{256, 2, 1, 13.0, 1.30, 1.05}, {128, 2, 2, 5.5, 0.79, 0.50}, {128, 4, 1, 5.0, 0.50, 0.50}, {64, 2, 4, 3.5, 0.68, 0.30}, {64, 4, 2, 3.0, 0.38, 0.21}};
+
+// The form and the split of the reduction (where tiles alone leave compute units idle) with the least expected time.
 GemmPlan plan_gemm(int64_t rows, int64_t cols, int64_t K, int planes) {
     GemmPlan best{};
     best.us = 1e30;
     const int64_t steps = (K + lin::BK - 1) / lin::BK;
-    for (const TileCost& c : kTiles) {
-        const int64_t ti = (rows + c.tile - 1) / c.tile, tj = (cols + c.tile - 1) / c.tile, tiles = ti * tj;
-        if (tiles > 0x7fffffff) continue;
-        for (int64_t want = 1; want <= 1024; want *= 2) {
-            const int64_t most = steps < want ? steps : want, per = (steps + most - 1) / most, splits = (steps + per - 1) / per;
-            if (splits * 2 <= want && want > 1) break;
+    const double products = planes == 3 ? 6.0 : 1.0;
+    for (const Form& f : kForms) {
+        const int64_t ti = (rows + f.tile - 1) / f.tile, tj = (cols + f.tile - 1) / f.tile, tiles = ti * tj;
+        int64_t last = 0;
+        for (int64_t want = 1; want <= 1024; want += want < 4 ? 1 : want / 4) {
+            const int64_t per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
+            if (splits == last) continue;
+            last = splits;
             const double part = (splits > 1 || planes > 1) ? 4.0 * splits * rows * cols : 0.0;
-            if (splits > 1 && part > 256e6) break;
-            if (tiles * splits > 0x7fffffff) break;
-            const double all = (double)tiles * splits, rounds = ceil(all / (256.0 * c.resident)), fill = all / 256.0;
-            const double load = fill <= 1.0 ? c.alone : fill >= c.resident ? rounds * c.resident * c.step : fill * c.step > c.alone ? fill * c.step : c.alone;
-            const double us = load * (double)(per * (planes == 3 ? 6 : 1)) / 2.2e3 + (part > 0 ? 4.0 + 2.0 * part / 5e6 : 0.0) + 4.0;
-            if (us < best.us) {
-                best.us = us;
-                best.tile = c.tile; best.tiles_i = (int)ti; best.tiles_j = (int)tj;
-                best.steps = (int)steps; best.splits = (int)splits; best.per_split = (int)per;
-            }
+            if (tiles * splits > 0x7fffffff || (splits > 1 && part > 256e6)) break;
+            const double load = (double)tiles * splits / 256.0, rounds = ceil(load / f.resident);
+            double step = f.step;
+            if (load <= 1.0) step = f.alone;
+            else if (load < f.resident) step = f.alone + (f.step - f.alone) * (load - 1.0) / (f.resident - 1.0);
+            const double work = rounds * f.round + (rounds > 1.0 ? load / f.resident * 0.5 + rounds * 0.5 : 1.0) * step * (double)per * products;
+            const double us = work + (part > 0.0 ? 4.0 + 2.0 * part / 5e6 : 0.0);
+            if (us < best.us) best = GemmPlan{f.tile, f.bufs, (int)ti, (int)tj, (int)steps, (int)splits, (int)per, us};
         }
     }
     return best;
@@ -322,6 +324,7 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
     GemmPlan g = plan_gemm(c.rows, c.cols, c.K, planes);
     if (c.a_ld >= far / 4 || c.b_ld >= far / 4) {          // (a tile of 256 rows would span 2^31 bytes)
         g.tile = 64;
+        g.bufs = 4;
         g.tiles_i = (int)((c.rows + 63) / 64);
         g.tiles_j = (int)((c.cols + 63) / 64);
     }
@@ -354,7 +357,13 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
     hipError_t e;
     {
         ProbeScope probe(st);
-        e = g.tile == 256 ? lin::gemm_256(p, c.a_in, c.b_in, act, st) : g.tile == 128 ? lin::gemm_128(p, c.a_in, c.b_in, act, st) : lin::gemm_64(p, c.a_in, c.b_in, act, st);
+        switch (g.tile * 10 + g.bufs) {
+            case 2562: e = lin::gemm_256_2(p, c.a_in, c.b_in, act, st); break;
+            case 1282: e = lin::gemm_128_2(p, c.a_in, c.b_in, act, st); break;
+            case 1284: e = lin::gemm_128_4(p, c.a_in, c.b_in, act, st); break;
+            case 642: e = lin::gemm_64_2(p, c.a_in, c.b_in, act, st); break;
+            default: e = lin::gemm_64_4(p, c.a_in, c.b_in, act, st); break;
+        }
     }
     if (e != hipSuccess || !second) return e;
     JoinParams q{p.part, f, a, b, p.rows, p.cols, p.K, p.splits, 1};

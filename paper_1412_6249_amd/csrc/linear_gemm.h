@@ -143,7 +143,7 @@ struct Shape {
     static constexpr int A_SKEW = 32, B_SKEW = 64;
     typedef Operand<BI, AIN, false, A_SKEW> A;
     typedef Operand<BJ, BIN, true, B_SKEW> B;
-    static constexpr int A_BYTES = A::S::BYTES, STAGE = A_BYTES + B::S::BYTES, LDS = 2 * STAGE;
+    static constexpr int A_BYTES = A::S::BYTES, STAGE = A_BYTES + B::S::BYTES;
     static constexpr int TI = BI / 32, TJ = BJ / 32;
 };
 
@@ -305,8 +305,9 @@ __device__ __forceinline__ void tile_of(const GemmParams& p, int& ti, int& tj, i
 }
 
 // EPI: PART; with B's reduction inner, act of y = act(. + bias) + res; else act of the slope that the sum is multiplied with.
-template <int BI, int BJ, bool AIN, bool BIN, int EPI>
-__global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear_gemm_kernel(const GemmParams p) {
+// BUFS: steps in LDS, all but the one in use on their way.
+template <int BI, int BJ, int BUFS, bool AIN, bool BIN, int EPI>
+__global__ __launch_bounds__(256, BI * BUFS > 256 ? 1 : BI * BUFS > 128 ? 2 : 4) void linear_gemm_kernel(const GemmParams p) {
     typedef Shape<BI, BJ, AIN, BIN> T;
     constexpr int TI = T::TI, TJ = T::TJ;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -384,29 +385,32 @@ __global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear
     // two sets of fragments: one is multiplied while the other is read
     Frag<AIN> fa[2][TI];
     Frag<BIN> fb[2][TJ];
-    // this wavefront's loads have landed and its LDS reads are done; then all meet
-    auto meet = [&]() {
+    // this wavefront's loads have landed, all but those of the `YOUNGER` last steps, and its LDS reads are done; then all meet
+    auto meet = [&](auto YOUNGER) {
+        constexpr int n = decltype(YOUNGER)::value * LOADS;
+        static_assert(n < 64, "the counter's range");
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0) lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt(0x0070 | (n & 15) | (n >> 4) << 14);        // vmcnt(n) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    typedef std::integral_constant<int, 0> None;
     auto a_at = [&](int buf, int kk) { return lds + buf * T::STAGE + T::A::half_at(a_frag, kk); };
     auto b_at = [&](int buf, int kk) { return lds + buf * T::STAGE + T::A_BYTES + T::B::half_at(b_frag, kk); };
 
-    request(0);
-    meet();
-    request(1);
+    each<BUFS>([&](auto B_) { request(B_.value); });
+    meet(std::integral_constant<int, BUFS - 1>());
     each<TI>([&](auto I) {
         read_now<T::A::tile_at(I.value), T::A::HALF>(fa[0][I.value], a_at(0, 0));
         read_now<T::B::tile_at(I.value), T::B::HALF>(fb[0][I.value], b_at(0, 0));
         settle<I.value>(acc);
     });
-    for (int s = 0, buf = 0; s < total; ++s, buf ^= 1) {
-        const int a1 = a_at(buf, 1), b1 = b_at(buf, 1), a0 = a_at(buf ^ 1, 0), b0 = b_at(buf ^ 1, 0);
+    for (int s = 0, buf = 0; s < total; ++s) {
+        const int other = buf + 1 == BUFS ? 0 : buf + 1;
+        const int a1 = a_at(buf, 1), b1 = b_at(buf, 1), a0 = a_at(other, 0), b0 = b_at(other, 0);
         const Request none[4] = {};
         each<TI / 2>([&](auto I) { block<T, AIN, BIN, false, 2 * I.value>(acc, fa[0], fb[0], fa[1], fb[1], a1, b1, none); });
-        meet();                                    // step s + 1 is in the other buffer, and nobody reads this one any more
+        meet(std::integral_constant<int, BUFS - 2>());     // step s + 1 is in the next buffer, and nobody reads this one any more
         begin_request(buf);
         each<TI / 2>([&](auto I) {
             constexpr int i = 4 * I.value;
@@ -416,9 +420,10 @@ __global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear
             block<T, AIN, BIN, true, 2 * I.value>(acc, fa[1], fb[1], fa[0], fb[0], a0, b0, q);
         });
         end_request();
+        buf = other;
     }
     each<TI>([&](auto I) { settle<I.value>(acc); });
-    meet();                                        // (the loads past the end wrote zeros) LDS is free
+    meet(None());                                  // (the loads past the end wrote zeros) LDS is free
 
     // Results: through LDS into rows, so that a lane has eight columns of one row and a few lanes whole lines of memory. The loop over them is a
     // loop: unrolled over the accumulators, every tile fetched 40 KB of instructions anew (22 - 44 us a tile).
@@ -527,47 +532,49 @@ __global__ __launch_bounds__(256, BI == 256 ? 1 : BI == 128 ? 2 : 4) void linear
     });
 }
 
-template <int BI, int BJ, bool AIN, bool BIN, int EPI>
+template <int BI, int BJ, int BUFS, bool AIN, bool BIN, int EPI>
 hipError_t launch_gemm(const GemmParams& p, hipStream_t st) {
-    typedef Shape<BI, BJ, AIN, BIN> T;
+    constexpr int LDS = Shape<BI, BJ, AIN, BIN>::STAGE * BUFS;
     const int64_t grid = (int64_t)p.tiles_i * p.tiles_j * p.splits;
     if (grid < 1 || grid > 0x7fffffff) return hipErrorInvalidValue;
-    const auto kernel = &linear_gemm_kernel<BI, BJ, AIN, BIN, EPI>;
-    if (T::LDS > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
+    const auto kernel = &linear_gemm_kernel<BI, BJ, BUFS, AIN, BIN, EPI>;
+    if (LDS > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), T::LDS, st, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), LDS, st, p);
     return hipGetLastError();
 }
 
-// One tile extent's kernels (linear_gemm_<tile>.hip). act: PART or an activation.
-hipError_t gemm_256(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st);
-hipError_t gemm_128(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st);
-hipError_t gemm_64(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st);
+// One tile extent's kernels, with two steps in LDS or four (linear_gemm_<tile>_<steps>.hip). act: PART or an activation.
+hipError_t gemm_256_2(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st);
+hipError_t gemm_128_2(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st);
+hipError_t gemm_128_4(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st);
+hipError_t gemm_64_2(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st);
+hipError_t gemm_64_4(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st);
 
-template <int BI, int BJ>
+template <int BI, int BJ, int BUFS>
 hipError_t gemm_any(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st) {
     if (a_in && b_in) {
         switch (act) {
-            case PART: return launch_gemm<BI, BJ, true, true, PART>(p, st);
-            case PURINE_ACT_NONE: return launch_gemm<BI, BJ, true, true, PURINE_ACT_NONE>(p, st);
-            case PURINE_ACT_RELU: return launch_gemm<BI, BJ, true, true, PURINE_ACT_RELU>(p, st);
-            case PURINE_ACT_SILU: return launch_gemm<BI, BJ, true, true, PURINE_ACT_SILU>(p, st);
-            case PURINE_ACT_GELU: return launch_gemm<BI, BJ, true, true, PURINE_ACT_GELU>(p, st);
-            case PURINE_ACT_GELU_TANH: return launch_gemm<BI, BJ, true, true, PURINE_ACT_GELU_TANH>(p, st);
+            case PART: return launch_gemm<BI, BJ, BUFS, true, true, PART>(p, st);
+            case PURINE_ACT_NONE: return launch_gemm<BI, BJ, BUFS, true, true, PURINE_ACT_NONE>(p, st);
+            case PURINE_ACT_RELU: return launch_gemm<BI, BJ, BUFS, true, true, PURINE_ACT_RELU>(p, st);
+            case PURINE_ACT_SILU: return launch_gemm<BI, BJ, BUFS, true, true, PURINE_ACT_SILU>(p, st);
+            case PURINE_ACT_GELU: return launch_gemm<BI, BJ, BUFS, true, true, PURINE_ACT_GELU>(p, st);
+            case PURINE_ACT_GELU_TANH: return launch_gemm<BI, BJ, BUFS, true, true, PURINE_ACT_GELU_TANH>(p, st);
         }
     } else if (a_in) {
         switch (act) {
-            case PART: return launch_gemm<BI, BJ, true, false, PART>(p, st);
-            case PURINE_ACT_NONE: return launch_gemm<BI, BJ, true, false, PURINE_ACT_NONE>(p, st);
-            case PURINE_ACT_RELU: return launch_gemm<BI, BJ, true, false, PURINE_ACT_RELU>(p, st);
-            case PURINE_ACT_SILU: return launch_gemm<BI, BJ, true, false, PURINE_ACT_SILU>(p, st);
-            case PURINE_ACT_GELU: return launch_gemm<BI, BJ, true, false, PURINE_ACT_GELU>(p, st);
-            case PURINE_ACT_GELU_TANH: return launch_gemm<BI, BJ, true, false, PURINE_ACT_GELU_TANH>(p, st);
+            case PART: return launch_gemm<BI, BJ, BUFS, true, false, PART>(p, st);
+            case PURINE_ACT_NONE: return launch_gemm<BI, BJ, BUFS, true, false, PURINE_ACT_NONE>(p, st);
+            case PURINE_ACT_RELU: return launch_gemm<BI, BJ, BUFS, true, false, PURINE_ACT_RELU>(p, st);
+            case PURINE_ACT_SILU: return launch_gemm<BI, BJ, BUFS, true, false, PURINE_ACT_SILU>(p, st);
+            case PURINE_ACT_GELU: return launch_gemm<BI, BJ, BUFS, true, false, PURINE_ACT_GELU>(p, st);
+            case PURINE_ACT_GELU_TANH: return launch_gemm<BI, BJ, BUFS, true, false, PURINE_ACT_GELU_TANH>(p, st);
         }
     } else if (!b_in) {
-        return act == PART ? launch_gemm<BI, BJ, false, false, PART>(p, st) : launch_gemm<BI, BJ, false, false, PURINE_ACT_NONE>(p, st);
+        return act == PART ? launch_gemm<BI, BJ, BUFS, false, false, PART>(p, st) : launch_gemm<BI, BJ, BUFS, false, false, PURINE_ACT_NONE>(p, st);
     }
     return hipErrorInvalidValue;
 }

@@ -1,0 +1,8 @@
+// Matrix products on tiles of 128 x 128 results, four steps of the reduction in LDS (linear_gemm.h).
+#include "linear_gemm.h"
+
+namespace purine {
+namespace lin {
+hipError_t gemm_128_4(const GemmParams& p, bool a_in, bool b_in, int act, hipStream_t st) { return gemm_any<128, 128, 4>(p, a_in, b_in, act, st); }
+}  // namespace lin
+}  // namespace purine
