@@ -1,37 +1,11 @@
 // Matrix product with bias, activation and residual in its epilogue, its gradients (purine_linear_*), and the gradient of an
 // activation by itself (purine_act_bwd).
+#include "linear_finish.h"
 #include "linear_gemm.h"
 #include "packets.h"
 
 namespace purine {
 namespace {
-
-template <typename T> __device__ __forceinline__ float widen(T v);
-template <> __device__ __forceinline__ float widen<float>(float v) { return v; }
-template <> __device__ __forceinline__ float widen<uint16_t>(uint16_t v) { return bf2f(v); }
-__device__ __forceinline__ void narrow(float v, float* p) { *p = v; }
-__device__ __forceinline__ void narrow(float v, uint16_t* p) { *p = f2bf(v); }
-
-// Element (i, k) of an operand at i * i_step + k * k_step.
-struct Source { const void* p; int64_t i_step, k_step; };
-
-// What the sum goes through on its way to memory (E: the operands' type).
-struct Finish {
-    const void* bias; const void* res; void* pre; const void* slope; void* out;
-    int64_t res_ld, pre_ld, slope_ld, out_ld;
-    int act, accumulate;
-};
-template <typename E, typename O>
-__device__ __forceinline__ void finish(const Finish& f, int64_t i, int j, float z) {
-    if (f.bias) z += widen<E>(((const E*)f.bias)[j]);
-    if (f.pre) narrow(z, (E*)f.pre + i * f.pre_ld + j);
-    if (f.slope) z *= slope_any(f.act, widen<E>(((const E*)f.slope)[i * f.slope_ld + j]));
-    else z = act_any(f.act, z);
-    if (f.res) z += widen<E>(((const E*)f.res)[i * f.res_ld + j]);
-    O* o = (O*)f.out + i * f.out_ld + j;
-    if (f.accumulate) z += widen<O>(*o);
-    narrow(z, o);
-}
 
 // Operands whose rows lie 2^24 elements apart or more, past the 32-bit offsets of the kernels on the matrix cores: 64 x 64 results per
 // workgroup, 16 per thread, fp32 products.
@@ -88,8 +62,7 @@ __global__ __launch_bounds__(256) void linear_pack_kernel(const T* __restrict__ 
 }
 
 // Adds the partial sums of the splits in order and finishes the results. A thread has V neighbouring columns of a row, and `lanes`
-// threads share the splits of one (few results of many splits: dw of a narrow layer over many positions). SPLIT3: sums of an fp32 product's parts, to be
-// scaled back; where one is infinite or NaN it is computed again as a plain fp32 sum.
+// threads share the splits of one (few results of many splits: dw of a narrow layer over many positions). SPLIT3: sums of an fp32 product's parts.
 struct JoinParams { const float* part; Finish f; Source a, b; int rows, cols, K, splits, lanes; };
 template <typename E, typename O, int V>
 __global__ __launch_bounds__(256) void linear_join_kernel(const JoinParams p) {
@@ -127,15 +100,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const JoinParams p) {
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         float z = v[e];
-        if constexpr (SPLIT3) {
-            z *= packets::JOIN_SCALE;
-            if (z - z != 0.0f) {
-                const float* a = (const float*)p.a.p + i * p.a.i_step;
-                const float* b = (const float*)p.b.p + (j + e) * p.b.i_step;
-                z = 0.0f;
-                for (int k = 0; k < p.K && z == z; ++k) z = fmaf(a[k * p.a.k_step], b[k * p.b.k_step], z);
-            }
-        }
+        if constexpr (SPLIT3) z = joined(z, p.a, p.b, i, j + e, p.K);
         finish<E, O>(p.f, i, j + e, z);
     }
 }
@@ -165,7 +130,7 @@ GemmPlan plan_gemm(int64_t rows, int64_t cols, int64_t K, int planes) {
             if (splits == last) continue;
             last = splits;
             const double part = (splits > 1 || planes > 1) ? 4.0 * splits * rows * cols : 0.0;
-            if (tiles * splits > 0x7fffffff || (splits > 1 && part > 256e6)) break;
+            if (tiles * splits > 0x7fffffff || (splits > 1 && (part > 256e6 || tiles * splits > 4096))) break;
             const double load = (double)tiles * splits / 256.0, rounds = ceil(load / f.resident);
             double step = f.step;
             if (load <= 1.0) step = f.alone;
@@ -176,6 +141,35 @@ GemmPlan plan_gemm(int64_t rows, int64_t cols, int64_t K, int planes) {
         }
     }
     return best;
+}
+
+// Products that one launch without scratch computes faster than the kernels above, by the measured times of both (us): a launch, steps of 32 in
+// each of the workgroup's wavefronts, alone on a compute unit or beside `load` others.
+DirectForm direct_form(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_in, int dtype) {
+    const bool f32 = dtype == PURINE_F32;
+    const int64_t steps = (K + 31) / 32;
+    double best = 1e30;
+    DirectForm form = DIRECT_NONE;
+    auto offer = [&](DirectForm f, double us) { if (us < best) { best = us; form = f; } };
+    // (a wavefront works on two groups of `depth` steps in turn, whether they exist or not)
+    auto chain = [&](int64_t groups, int64_t waves, int64_t depth, double alone, double full) {
+        const double load = (double)groups / 256.0;
+        const int64_t each = ((steps + waves - 1) / waves + 2 * depth - 1) / (2 * depth) * (2 * depth);
+        return 3.8 + (double)each * fmax(alone, full * load) + 0.4 * load;
+    };
+    if (a_in && b_in) {
+        if (rows <= 4 && K % (f32 ? 4 : 8) == 0) offer(DIRECT_ROW, 4.0 + (double)cols * (double)K * (f32 ? 4.0 : 2.0) / (rows > 2 && !f32 ? 3.6e6 : 5.0e6));
+        if (rows <= 16) offer(DIRECT_ROWS, chain((cols + 15) / 16, 8, 4, f32 ? 0.75 : 0.29, f32 ? 1.08 : 0.47));
+    }
+    const int64_t groups = ((rows + 31) / 32) * ((cols + 31) / 32);
+    if (groups <= 0x7fffffff)
+        offer(DIRECT_SMALL, f32 ? chain(groups, 4, 1, 0.85, 0.95) : a_in && b_in ? chain(groups, 4, 2, 0.36, 0.36) : a_in ? chain(groups, 4, 1, 0.44, 0.55) :
+                            chain(groups, 4, 1, 0.60, 0.62));
+    if (best < 6.0) return form;                   // (as short as any launch)
+    // the kernels above, with the launches that lay operands out and that join sums
+    auto laid = [&](int64_t n, bool in) { return f32 || (in ? K : n) % 8 ? 3.0 + (double)n * (double)K * (f32 ? 10.0 : 4.0) / 4.5e6 : 0.0; };
+    if (plan_gemm(rows, cols, K, f32 ? 3 : 1).us + 2.0 + laid(rows, a_in) + laid(cols, b_in) <= best) return DIRECT_NONE;
+    return form;
 }
 
 int64_t packed_ld(int64_t len) { return (len + 7) / 8 * 8; }
@@ -270,6 +264,7 @@ int act_rows(int64_t N, int64_t K) {
 }  // namespace
 
 size_t linear_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_in, int dtype) {
+    if (direct_form(rows, cols, K, a_in, b_in, dtype) != DIRECT_NONE) return 0;
     const int planes = dtype == PURINE_F32 ? 3 : 1;
     const GemmPlan g = plan_gemm(rows, cols, K, planes);
     size_t n = 0;
@@ -280,8 +275,6 @@ size_t linear_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_
 }
 
 namespace {
-
-Source source_of(const void* p, int64_t ld, bool in) { return {p, in ? ld : 1, in ? 1 : ld}; }
 
 template <typename E, typename O>
 hipError_t join(const JoinParams& q, hipStream_t st) {
@@ -308,11 +301,14 @@ void pack(const void* src, int64_t ld, void* dst, int64_t rows, int64_t K, bool 
 hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
     const bool f32 = c.dtype == PURINE_F32;
     const int planes = f32 ? 3 : 1;
-    Finish f{c.bias, c.res, c.pre, c.slope, c.out, c.res_ld, c.pre_ld, c.slope_ld, c.out_ld, c.act, c.accumulate};
+    const Finish f = finish_of(c);
     const Source a = source_of(c.a, c.a_ld, c.a_in), b = source_of(c.b, c.b_ld, c.b_in);
     (void)hipGetLastError();
-    const int64_t far = (int64_t)1 << 24;
-    if (c.a_ld >= far || c.b_ld >= far) {
+    const DirectForm direct = direct_form(c.rows, c.cols, c.K, c.a_in, c.b_in, c.dtype);
+    const int64_t far = (int64_t)1 << 24, es = f32 ? 4 : 2;
+    const int64_t span = ((c.a_in ? c.rows : c.K) * c.a_ld > (c.b_in ? c.cols : c.K) * c.b_ld ? (c.a_in ? c.rows : c.K) * c.a_ld : (c.b_in ? c.cols : c.K) * c.b_ld) * es;
+    if (direct != DIRECT_NONE && span < 0x7fffffff) return launch_linear_direct(c, direct, st);
+    if (direct != DIRECT_NONE || c.a_ld >= far || c.b_ld >= far) {
         FarParams p{a, b, f, (int)c.rows, (int)c.cols, (int)c.K, (int)((c.cols + TS - 1) / TS)};
         const unsigned grid = (unsigned)((c.rows + TS - 1) / TS * p.tiles_j);
         ProbeScope probe(st);
