@@ -4,8 +4,8 @@
 //     w = w (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
 //
 // Bound: HBM, every tensor read once and written once. The table of tensors travels in the kernel arguments, 40 tensors a launch,
-// so that a step needs no memory of its own; a workgroup takes 2048 consecutive elements of one tensor, found from the first
-// workgroups' numbers in the table.
+// so that a step needs no memory of its own; a workgroup takes 2048 consecutive elements of one tensor, found from the tensors' first
+// workgroups in the table.
 #include <math.h>
 
 #include "bf16.h"
@@ -21,10 +21,11 @@ struct AdamwTensor {
     void* w; const void* dw; void* m; void* v;
     float* ms; float* vs;
     uint16_t* copy;
-    unsigned n, first;         // elements; first workgroup
+    unsigned n;
 };
 struct AdamwParams {
     AdamwTensor t[TABLE];
+    unsigned first[TABLE];     // tensors' first workgroups
     const int* done;           // steps done before, or null: `step` is this one
     float decay, lr, beta1, beta1c, beta2, beta2c, eps, grad_scale;
     float log1, log2;          // log beta
@@ -152,11 +153,12 @@ __device__ __forceinline__ void put_codes(uint8_t* p, int left, uint2 c) {
 
 template <typename W, typename D, bool CODED>
 __global__ __launch_bounds__(NT) void adamw_kernel(const AdamwParams p) {
-    int k = 0;
-    for (int hop = 32; hop; hop >>= 1)          // the last tensor that begins at or before this workgroup
-        if (k + hop < p.count && p.t[k + hop].first <= blockIdx.x) k += hop;
+    // the last tensor that begins at or before this workgroup: one load for the wavefront (a search by halves is six, one after the other)
+    const int lane = threadIdx.x & 63;
+    const bool before = lane < p.count && p.first[lane < TABLE ? lane : 0] <= blockIdx.x;
+    const int k = __builtin_amdgcn_readfirstlane(__popcll(__ballot(before)) - 1);
     const AdamwTensor& t = p.t[k];
-    const unsigned at = (blockIdx.x - t.first) * CHUNK + threadIdx.x * PER;
+    const unsigned at = (blockIdx.x - p.first[k]) * CHUNK + threadIdx.x * PER;
     const int left = at < t.n ? (int)min(t.n - at, (unsigned)PER) : 0;
     float step_size = p.step_size, v_scale = p.v_scale;
     unsigned step = p.step;
@@ -271,7 +273,7 @@ hipError_t launch_adamw(const purine_adamw_desc& d, const purine_adamw_param* pa
             o.ms = coded ? (float*)q.m_scale.data : nullptr;
             o.vs = coded ? (float*)q.v_scale.data : nullptr;
             o.n = (unsigned)elements(q.w);
-            o.first = grid;
+            p.first[i] = grid;
             grid += (o.n + CHUNK - 1) / CHUNK;
         }
         const bool w16 = params[from].w.dtype == PURINE_BF16, d16 = params[from].dw.dtype == PURINE_BF16;

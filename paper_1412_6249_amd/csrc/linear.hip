@@ -234,20 +234,25 @@ __global__ __launch_bounds__(ANT) void act_bwd_kernel(const ActParams p) {
 #pragma unroll
     for (int e = 0; e < V; ++e) o[e] = sum[e];
 }
-// 16 columns per workgroup, the slices over 16 threads each.
+// Four columns per workgroup, the slices over 64 threads each.
+constexpr int CS = 4;
 template <typename O>
 __global__ __launch_bounds__(256) void column_sums_kernel(const float* part, O* db, int slices, int K, int accumulate) {
-    __shared__ float sums[16][17];
-    const int l = threadIdx.x & 15, r = threadIdx.x >> 4, j = blockIdx.x * 16 + l;
+    __shared__ float sums[256 / CS][CS + 1];
+    const int l = threadIdx.x % CS, r = threadIdx.x / CS, j = blockIdx.x * CS + l;
     float sum = 0.0f;
     if (j < K) {
-#pragma unroll 4
-        for (int s = r; s < slices; s += 16) sum += part[(size_t)s * K + j];
+#pragma unroll 8
+        for (int s = r; s < slices; s += 256 / CS) sum += part[(size_t)s * K + j];
     }
     sums[r][l] = sum;
     __syncthreads();
+    for (int half = 128 / CS; half; half /= 2) {
+        if (r < half) sums[r][l] += sums[r + half][l];
+        __syncthreads();
+    }
     if (r || j >= K) return;
-    for (int k = 1; k < 16; ++k) sum += sums[k][l];
+    sum = sums[0][l];
     if (accumulate) sum += widen<O>(db[j]);
     narrow(sum, db + j);
 }
@@ -402,7 +407,7 @@ hipError_t launch_act_bwd(int dtype, const void* pre, int64_t pre_ld, const void
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !db) return e;
-    const unsigned grid = (unsigned)((K + 15) / 16);
+    const unsigned grid = (unsigned)((K + CS - 1) / CS);
     if (db_dtype == PURINE_F32) hipLaunchKernelGGL((column_sums_kernel<float>), dim3(grid), dim3(256), 0, st, p.part, (float*)db, p.slices, (int)K, accumulate);
     else hipLaunchKernelGGL((column_sums_kernel<uint16_t>), dim3(grid), dim3(256), 0, st, p.part, (uint16_t*)db, p.slices, (int)K, accumulate);
     return hipGetLastError();
