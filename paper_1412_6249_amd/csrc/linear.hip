@@ -256,13 +256,13 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const float* part, O* 
     if (accumulate) sum += widen<O>(db[j]);
     narrow(sum, db + j);
 }
-// Rows of a slice: some 1024 workgroups, and few enough slices that their sums are a small part of the matrix; 16 rows per thread at least.
-int act_rows(int64_t N, int64_t K) {
-    const int64_t vectors = (K + 7) / 8, tiles = (vectors + ANT - 1) / ANT, R = vectors < ANT ? ANT / vectors : 1;
+// Rows of a slice where threads own V columns: some 1024 workgroups, and one batch of loads per thread at least.
+int act_rows(int64_t N, int64_t K, int V) {
+    const int64_t vectors = (K + V - 1) / V, tiles = (vectors + ANT - 1) / ANT, R = vectors < ANT ? ANT / vectors : 1;
     int64_t slices = 1024 / tiles;
     if (slices < 1) slices = 1;
     int64_t rows = (N + slices - 1) / slices;
-    if (rows < 8 * R) rows = 8 * R;
+    if (rows < 4 * R) rows = 4 * R;
     return (int)(rows < N ? rows : N);
 }
 
@@ -373,7 +373,11 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
 }
 
 size_t act_bwd_ws_bytes(int64_t N, int64_t K) {
-    const int64_t rows = act_rows(N, K), slices = (N + rows - 1) / rows;
+    int64_t slices = 0;
+    for (int V : {1, 4, 8}) {
+        const int64_t rows = act_rows(N, K, V), n = (N + rows - 1) / rows;
+        if (n > slices) slices = n;
+    }
     return (size_t)slices * K * 4;
 }
 
@@ -395,15 +399,16 @@ void act_bwd(const ActParams& q, int act, hipStream_t st) {
 
 hipError_t launch_act_bwd(int dtype, const void* pre, int64_t pre_ld, const void* dy, int64_t dy_ld, void* g, int64_t g_ld, void* db, int db_dtype,
                           bool accumulate, int64_t N, int64_t K, int act, void* ws, hipStream_t st) {
-    ActParams p{pre, dy, g, db ? (float*)ws : nullptr, pre_ld, dy_ld, g_ld, (int)N, (int)K, act_rows(N, K), 0, 1};
-    p.slices = (int)((N + p.rows - 1) / p.rows);
     if (!pre) act = PURINE_ACT_NONE;
     const int64_t all = K | dy_ld | (pre ? pre_ld : 0) | (g ? g_ld : 0);
+    const int V = dtype == PURINE_F32 ? (all % 4 ? 1 : 4) : all % 8 ? 1 : 8;
+    ActParams p{pre, dy, g, db ? (float*)ws : nullptr, pre_ld, dy_ld, g_ld, (int)N, (int)K, act_rows(N, K, V), 0, 1};
+    p.slices = (int)((N + p.rows - 1) / p.rows);
     (void)hipGetLastError();
     {
         ProbeScope probe(st);
-        if (dtype == PURINE_F32) all % 4 == 0 ? act_bwd<float, 4>(p, act, st) : act_bwd<float, 1>(p, act, st);
-        else all % 8 == 0 ? act_bwd<uint16_t, 8>(p, act, st) : act_bwd<uint16_t, 1>(p, act, st);
+        if (dtype == PURINE_F32) V == 4 ? act_bwd<float, 4>(p, act, st) : act_bwd<float, 1>(p, act, st);
+        else V == 8 ? act_bwd<uint16_t, 8>(p, act, st) : act_bwd<uint16_t, 1>(p, act, st);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !db) return e;
