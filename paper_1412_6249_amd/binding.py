@@ -86,6 +86,7 @@ except ImportError as e:
     raise ImportError("_marshal.so, the native half of this module, is not built or was built against another PyTorch: run "
                       "`python -c 'import __graft_entry__ as g; g.build()'` (or paper_1412_6249_amd/build.py) first") from e
 _marshal.descriptor_types(purine_conv_desc, purine_pool_desc)
+_marshal.adamw_types(purine_adamw_desc, purine_adamw_param)
 
 _P = ctypes.POINTER
 _T, _D, _PD = _P(purine_tensor), _P(purine_conv_desc), _P(purine_pool_desc)
@@ -579,7 +580,10 @@ def adamw_params(w, dw, m, v, m_scale=None, v_scale=None, copy=None):
 
 def purine_adamw_step(desc, params, done=None, stream=None):
     """params: what adamw_params returned. done: int32 tensor of one element with the steps done before, or None."""
-    _check(_lib.purine_adamw_step(_ref(desc), params.array, len(params), _opt(done), _stream(stream)), "purine_adamw_step")
+    rc = _marshal.purine_adamw_step(desc, params.array, done, stream)
+    if rc is None:
+        rc = _lib.purine_adamw_step(_ref(desc), params.array, len(params), _opt(done), _stream(stream))
+    _check(rc, "purine_adamw_step")
 
 
 def purine_bias_fwd(b, y, stream=None):

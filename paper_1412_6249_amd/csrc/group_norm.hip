@@ -643,10 +643,8 @@ unsigned held_grid(NormParams& p, const HeldPlan& h) {
 
 }  // namespace
 
-size_t group_norm_ws_bytes(bool backward, int64_t N, int64_t S, int64_t C, int64_t G, int dtype) {
-    const bool held = held_plan(N, S, C, G, dtype, vector_of(C, dtype), backward).width != 0;
-    return held ? (backward ? (size_t)(N * C) * sizeof(float2) : 0) : (size_t)(N * slices_of(N, S, C) * C) * sizeof(float2);
-}
+// What the sliced kernels take, whichever a call gets (the held ones need a slice's at most).
+size_t group_norm_ws_bytes(int64_t N, int64_t S, int64_t C) { return (size_t)(N * slices_of(N, S, C) * C) * sizeof(float2); }
 
 hipError_t launch_group_norm_fwd(int dtype, const NormShape& s, const void* x, const float* scale, const float* shift, void* y, float* mean,
                                  float* rstd, void* ws, hipStream_t st) {

@@ -4,10 +4,11 @@
 // Bound: host time per call. A descriptor made with ctypes costs 1.6 us, a call with five tensors and its stream about
 // 10, more than its launches: most small layers were bound by it. Here an argument costs tens of nanoseconds.
 //
-// Every function takes its entry point's arguments in the C order (scratch and its size as one argument) and returns the
+// Every function takes its entry point's arguments in the C order (scratch and its size as one argument, a table and its length too) and returns the
 // status, or None for any argument that is not the plain case (a tensor's descriptor made by hand, another kind of object, a
 // tensor that the operators refuse): the caller then takes the general path, which says what is wrong. Convolution and
-// pooling descriptors are instances of the two ctypes structures that descriptor_types() is given, as ctypes itself asks.
+// pooling descriptors are instances of the two ctypes structures that descriptor_types() is given, as ctypes itself asks; those of the AdamW
+// step, and its tables, are of the two that adamw_types() is given.
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
@@ -34,9 +35,12 @@ struct Call {
     void* ws = nullptr;
     size_t ws_bytes = 0;
     bool ws_taken = false;
-    Py_buffer desc{};
+    Py_buffer desc{}, table{};
     bool ok = true;                          // the plain case so far
-    ~Call() { if (desc.obj) PyBuffer_Release(&desc); }
+    ~Call() {
+        if (desc.obj) PyBuffer_Release(&desc);
+        if (table.obj) PyBuffer_Release(&table);
+    }
     PyObject* arg() {
         if (next >= n) { ok = false; return nullptr; }
         return args[next++];
@@ -44,8 +48,18 @@ struct Call {
 };
 
 PyTypeObject* descriptor_type[2] = {nullptr, nullptr};     // purine_conv_desc, purine_pool_desc
+PyTypeObject* adamw_type[2] = {nullptr, nullptr};          // purine_adamw_desc, purine_adamw_param
 
 bool is_descriptor(PyObject* o, int which) { return descriptor_type[which] && PyObject_TypeCheck(o, descriptor_type[which]); }
+
+// a ctypes array of purine_adamw_param
+bool is_table(PyObject* o) {
+    PyObject* type = PyObject_GetAttrString((PyObject*)Py_TYPE(o), "_type_");
+    const bool is = type && type == (PyObject*)adamw_type[1] && PyObject_HasAttrString((PyObject*)Py_TYPE(o), "_length_");    // (no pointer)
+    PyErr_Clear();
+    Py_XDECREF(type);
+    return is;
+}
 
 bool fill(purine_tensor& d, PyObject* o, bool rows) {
     if (!THPVariable_Check(o)) return false;
@@ -89,12 +103,22 @@ A take(Call& c) {
         if (!c.ok || !is_descriptor(o, which) || PyObject_GetBuffer(o, &c.desc, PyBUF_SIMPLE) != 0) { PyErr_Clear(); c.ok = false; return nullptr; }
         if (c.desc.len < (Py_ssize_t)sizeof(std::remove_pointer_t<A>)) c.ok = false;
         return (A)c.desc.buf;
+    } else if constexpr (std::is_same_v<A, const purine_adamw_desc*>) {
+        PyObject* o = c.arg();
+        if (!c.ok || !adamw_type[0] || !PyObject_TypeCheck(o, adamw_type[0]) || PyObject_GetBuffer(o, &c.desc, PyBUF_SIMPLE) != 0 ||
+            c.desc.len < (Py_ssize_t)sizeof(purine_adamw_desc)) { PyErr_Clear(); c.ok = false; return nullptr; }
+        return (A)c.desc.buf;
+    } else if constexpr (std::is_same_v<A, const purine_adamw_param*>) {
+        PyObject* o = c.arg();                                          // an array of them, whose length is the next argument
+        if (!c.ok || !is_table(o) || PyObject_GetBuffer(o, &c.table, PyBUF_SIMPLE) != 0) { PyErr_Clear(); c.ok = false; return nullptr; }
+        return (A)c.table.buf;
     } else if constexpr (std::is_same_v<A, float>) {
         PyObject* o = c.arg();
         const double v = c.ok ? PyFloat_AsDouble(o) : 0.0;
         if (PyErr_Occurred()) { PyErr_Clear(); c.ok = false; }
         return (float)v;
     } else if constexpr (std::is_same_v<A, int>) {
+        if (c.table.obj) return (int)(c.table.len / (Py_ssize_t)sizeof(purine_adamw_param));
         PyObject* o = c.arg();
         if (!c.ok || !PyLong_Check(o)) { c.ok = false; return 0; }      // (True and False are ints)
         int overflow = 0;
@@ -159,7 +183,7 @@ PyObject* invoke(int (*fn)(A...), PyObject* const* args, Py_ssize_t n, unsigned 
     X(purine_fc_fwd, 4) X(purine_fc_bwd_data, 0) X(purine_fc_bwd_weight, 8) X(purine_sgd_update, 0)                        \
     X(purine_bias_fwd, 0) X(purine_bias_bwd, 0) X(purine_relu_fwd, 0) X(purine_relu_bwd, 0)                                \
     X(purine_maxpool_fwd, 0) X(purine_maxpool_bwd, 0) X(purine_maxpool_bwd_relu, 0)                                       \
-    X(purine_group_norm_fwd, 54) X(purine_group_norm_bwd, 390)
+    X(purine_group_norm_fwd, 54) X(purine_group_norm_bwd, 390) X(purine_adamw_step, 1)
 ENTRIES(ENTRY)
 MATRIX_ENTRIES(MATRIX_ENTRY)
 
@@ -172,6 +196,19 @@ PyObject* descriptor_types(PyObject*, PyObject* const* args, Py_ssize_t n) {
         Py_INCREF(args[i]);
         Py_XDECREF((PyObject*)descriptor_type[i]);
         descriptor_type[i] = (PyTypeObject*)args[i];
+    }
+    Py_RETURN_NONE;
+}
+
+PyObject* adamw_types(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 2 || !PyType_Check(args[0]) || !PyType_Check(args[1])) {
+        PyErr_SetString(PyExc_TypeError, "adamw_types(purine_adamw_desc, purine_adamw_param)");
+        return nullptr;
+    }
+    for (int i = 0; i < 2; ++i) {
+        Py_INCREF(args[i]);
+        Py_XDECREF((PyObject*)adamw_type[i]);
+        adamw_type[i] = (PyTypeObject*)args[i];
     }
     Py_RETURN_NONE;
 }
@@ -189,6 +226,7 @@ PyObject* takes_descriptor(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define METHOD(NAME, OPTIONAL) {#NAME, (PyCFunction)(void (*)(void))&call_##NAME, METH_FASTCALL, nullptr},
 PyMethodDef methods[] = {ENTRIES(METHOD) MATRIX_ENTRIES(METHOD)
     {"descriptor_types", (PyCFunction)(void (*)(void))&descriptor_types, METH_FASTCALL, nullptr},
+    {"adamw_types", (PyCFunction)(void (*)(void))&adamw_types, METH_FASTCALL, nullptr},
     {"takes_descriptor", (PyCFunction)(void (*)(void))&takes_descriptor, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
