@@ -165,6 +165,7 @@ DirectForm direct_form(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_
     if (groups <= 0x7fffffff)
         offer(DIRECT_SMALL, f32 ? chain(groups, 4, 1, 0.85, 0.95) : a_in && b_in ? chain(groups, 4, 2, 0.36, 0.36) : a_in ? chain(groups, 4, 1, 0.44, 0.55) :
                             chain(groups, 4, 1, 0.60, 0.62));
+    if (!f32 && a_in && rows >= 4096 && stream_fits(cols, K)) offer(DIRECT_STREAM, stream_us(rows, cols, K));
     if (best < 6.0) return form;                   // (as short as any launch)
     // the kernels above, with the launches that lay operands out and that join sums
     auto laid = [&](int64_t n, bool in) { return f32 || (in ? K : n) % 8 ? 3.0 + (double)n * (double)K * (f32 ? 10.0 : 4.0) / 4.5e6 : 0.0; };
@@ -312,6 +313,7 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
     const DirectForm direct = direct_form(c.rows, c.cols, c.K, c.a_in, c.b_in, c.dtype);
     const int64_t far = (int64_t)1 << 24, es = f32 ? 4 : 2;
     const int64_t span = ((c.a_in ? c.rows : c.K) * c.a_ld > (c.b_in ? c.cols : c.K) * c.b_ld ? (c.a_in ? c.rows : c.K) * c.a_ld : (c.b_in ? c.cols : c.K) * c.b_ld) * es;
+    if (direct == DIRECT_STREAM) return launch_linear_stream(c, st);
     if (direct != DIRECT_NONE && span < 0x7fffffff) return launch_linear_direct(c, direct, st);
     if (direct != DIRECT_NONE || c.a_ld >= far || c.b_ld >= far) {
         FarParams p{a, b, f, (int)c.rows, (int)c.cols, (int)c.K, (int)((c.cols + TS - 1) / TS)};

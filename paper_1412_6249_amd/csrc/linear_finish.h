@@ -52,8 +52,12 @@ Finish finish_of(const LinearCall& c) { return {c.bias, c.res, c.pre, c.slope, c
 
 }  // namespace
 
-// Products in one launch (linear_direct.hip): few rows, small matrices.
-enum DirectForm { DIRECT_NONE = 0, DIRECT_ROW /* up to 4 rows, whole packets */, DIRECT_ROWS /* up to 16 */, DIRECT_SMALL };      // (the first two: both reductions inner)
+// Products in one launch (linear_direct.hip, linear_stream.hip): few rows, small matrices, many rows by a small matrix.
+enum DirectForm { DIRECT_NONE = 0, DIRECT_ROW /* up to 4 rows, whole packets */, DIRECT_ROWS /* up to 16 */, DIRECT_SMALL, DIRECT_STREAM };      // (the first two: both reductions inner)
 hipError_t launch_linear_direct(const LinearCall& c, DirectForm form, hipStream_t st);
+// bf16, A's reduction inner, whole packets
+bool stream_fits(int64_t cols, int64_t K);
+double stream_us(int64_t rows, int64_t cols, int64_t K);
+hipError_t launch_linear_stream(const LinearCall& c, hipStream_t st);
 
 }  // namespace purine

@@ -252,14 +252,17 @@ __device__ __forceinline__ void get8(const float* p, bool whole, int n, float (&
         for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.0f;
     }
 }
+__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float floatx2 __attribute__((ext_vector_type(2)));
+    u32x4 k;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { const floatx2 f = {v[2 * e], v[2 * e + 1]}; k[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2)); }
+    return k;
+}
 __device__ __forceinline__ void put8(uint16_t* p, bool whole, int n, const float (&v)[8]) {
     if (whole) {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        typedef float floatx2 __attribute__((ext_vector_type(2)));
-        u32x4 k;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { const floatx2 f = {v[2 * e], v[2 * e + 1]}; k[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2)); }
-        *reinterpret_cast<u32x4*>(p) = k;
+        *reinterpret_cast<u32x4*>(p) = pack8(v);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) if (e < n) p[e] = f2bf(v[e]);
