@@ -116,7 +116,9 @@ struct GemmPlan {
 struct Form { int tile, bufs, resident; double round, step, alone; };
 constexpr Form kForms[] = {{256, 2, 1, 13.0, 1.30, 1.05}, {128, 2, 2, 5.5, 0.79, 0.50}, {128, 4, 1, 5.0, 0.50, 0.50}, {64, 2, 4, 3.5, 0.68, 0.30}, {64, 4, 2, 3.0, 0.38, 0.21}};
 
-// The form and the split of the reduction (where tiles alone leave compute units idle) with the least expected time.
+// The form and the split of the reduction (where tiles alone leave compute units idle) with the least expected time. The compute units with the most
+// workgroups count; smaller tiles fetch an operand more often (a microsecond per 40 MB). us, weights from memory: 128 x 9216 x 4096 in tiles of 64 and 3 parts
+// of the reduction 38, 2 parts 33, in tiles of 128 and 8 parts 29.5; 256 x 4096 x 4096 in tiles of 64 23, of 128 and 4 parts 26.
 GemmPlan plan_gemm(int64_t rows, int64_t cols, int64_t K, int planes) {
     GemmPlan best{};
     best.us = 1e30;
@@ -134,9 +136,10 @@ GemmPlan plan_gemm(int64_t rows, int64_t cols, int64_t K, int planes) {
             const double load = (double)tiles * splits / 256.0, rounds = ceil(load / f.resident);
             double step = f.step;
             if (load <= 1.0) step = f.alone;
-            else if (load < f.resident) step = f.alone + (f.step - f.alone) * (load - 1.0) / (f.resident - 1.0);
+            else if (load < f.resident) step = f.alone + (f.step - f.alone) * (ceil(load) - 1.0) / (f.resident - 1.0);
+            const double read = 2.0 * products * (double)K * ((double)rows * (double)tj + (double)cols * (double)ti);
             const double work = rounds * f.round + (rounds > 1.0 ? load / f.resident * 0.5 + rounds * 0.5 : 1.0) * step * (double)per * products;
-            const double us = work + (part > 0.0 ? 4.0 + 2.0 * part / 5e6 : 0.0);
+            const double us = work + read / 40e6 + (part > 0.0 ? 4.0 + 2.0 * part / 5e6 : 0.0);
             if (us < best.us) best = GemmPlan{f.tile, f.bufs, (int)ti, (int)tj, (int)steps, (int)splits, (int)per, us};
         }
     }
