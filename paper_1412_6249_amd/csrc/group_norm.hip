@@ -412,11 +412,11 @@ __device__ __forceinline__ void join_held(const float (&s)[V], const float (&q)[
 template <typename T, int V, int ACT, int NV, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_held_kernel(const NormParams p) {
     __shared__ float2 sums[THREADS * V], chan[THREADS], stat[THREADS];
+    __shared__ float about[THREADS];           // the channels' values that the sums are taken about
     const int b = held_block(), n = b / p.tiles, c0 = (b - n * p.tiles) * p.width, cv = p.width / V, R = THREADS / cv;
     const int r = threadIdx.x / cv, c = c0 + (int)threadIdx.x % cv * V;
     const bool on = r < R;
-    const T* x0 = (const T*)p.x + n * p.x_ns;
-    const T* x = x0 + c;
+    const T* x = (const T*)p.x + n * p.x_ns + c;
     Pack<T, V> in[NV];
     float k[V], s[V], q[V];
 #pragma unroll
@@ -434,13 +434,14 @@ __global__ __launch_bounds__(THREADS) void norm_held_kernel(const NormParams p) 
             for (int i = 0; i < V; ++i) { const float d = v[i] - k[i]; s[i] += d; q[i] += d * d; }
         }
     }
+    if (r == 0)
+#pragma unroll
+        for (int i = 0; i < V; ++i) about[c - c0 + i] = k[i];
     join_held<V, THREADS>(s, q, sums, chan, p.width, R, on);
     for_groups<THREADS>(p.width / p.per, p.per, [&](int g, int lane, int lanes, auto&& sum) {
         const float2 o = group_stats(p, lane, lanes, sum, [&](int i, float& cs, float& cq, float& ck) {
             const float2 w = chan[g * p.per + i];
-            float v[1];
-            load_v<T, 1>(x0 + c0 + g * p.per + i, v);
-            cs = w.x; cq = w.y; ck = v[0];
+            cs = w.x; cq = w.y; ck = about[g * p.per + i];
         });
         if (lane == 0) {
             stat[g] = o;
@@ -485,16 +486,18 @@ __global__ __launch_bounds__(THREADS) void norm_grad_held_kernel(const NormParam
     if (on) {
         Pack<T, V> gr[NV];
         float sc[V], sh[V];
+        // (first: loads arrive in order, and every piece needs these)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int g = n * p.G + (c + i) / p.per;
+            mu[i] = p.mean[g]; rstd[i] = p.rstd[g]; sc[i] = scale_of(p, c + i); sh[i] = shift_of(p, c + i);
+        }
+        asm volatile("" ::: "memory");
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
             const int64_t row = (int64_t)min(r + u * R, p.S - 1) * p.C;
             in[u] = *reinterpret_cast<const Pack<T, V>*>(x + row);
             gr[u] = *reinterpret_cast<const Pack<T, V>*>(dy + row);
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int g = n * p.G + (c + i) / p.per;
-            mu[i] = p.mean[g]; rstd[i] = p.rstd[g]; sc[i] = scale_of(p, c + i); sh[i] = shift_of(p, c + i);
         }
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
