@@ -560,27 +560,37 @@ int vector_of(int64_t C, int dtype) {
     return 1;
 }
 
-// Channels of a workgroup that holds its share of an image in registers, and its pieces per thread; 0 where that does not apply. Whole
-// groups and whole pieces; as wide as fits up to a line of memory (128 bytes), unless that leaves fewer than 512 workgroups.
+// Channels of a workgroup that holds its share of an image in registers, its pieces per thread and its threads; no width where that does not apply.
+// Whole groups and whole pieces; as wide as fits up to a line of memory (128 bytes), unless that leaves fewer than 512 workgroups. Workgroups of
+// 256 threads where they hold 48 bytes of a row or more, else of 512: the more workgroups a compute unit has, the more their loads, sums and
+// stores overlap (us, bf16 forward: 256 x 196 x 256 in 128 bytes by 256 threads 15.6, by 512 19.7; 128 x 784 x 192 in 48 by 256 19.6, in 96 by 512 22.2; gradients gain 1
+// to 4%, those of fp32 lose as much).
 struct HeldPlan { int width, pieces, threads; };
 HeldPlan held_plan(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, int v, bool backward) {
     const int64_t per = C / G, bytes = dtype == PURINE_BF16 ? 2 : 4;
     int64_t unit = per;
     while (unit % v) unit += per;
-    HeldPlan best{0, 0, 0};
-    if (unit > C || C % unit) return best;
-    for (int64_t m = 1; unit * m <= C; ++m) {
-        const int64_t w = unit * m, cv = w / v;
-        if (C % w) continue;
-        if (w > 256 || cv > 256) break;
-        if (best.width && (w * bytes > 128 && best.width * bytes >= 64)) break;
-        if (best.width && N * (C / w) < 512) break;
-        const int threads = S * cv <= 256 * 4 ? 256 : HT;
-        const int64_t R = threads / cv, pieces = (S + R - 1) / R;
-        if (pieces > (backward && v == 8 ? HELD_GRAD : HELD)) break;
-        best = HeldPlan{(int)w, (int)pieces, threads};
+    if (unit > C || C % unit) return HeldPlan{0, 0, 0};
+    auto widest = [&](bool few) {
+        HeldPlan best{0, 0, 0};
+        for (int64_t m = 1; unit * m <= C; ++m) {
+            const int64_t w = unit * m, cv = w / v;
+            if (C % w) continue;
+            if (w > 256 || cv > 256) break;
+            if (best.width && (w * bytes > 128 && best.width * bytes >= 64)) break;
+            if (best.width && N * (C / w) < 512) break;
+            const int threads = few || S * cv <= 256 * 4 ? 256 : HT;
+            const int64_t R = threads / cv, pieces = (S + R - 1) / R;
+            if (pieces > (few || (backward && v == 8) ? HELD_GRAD : HELD)) break;
+            best = HeldPlan{(int)w, (int)pieces, threads};
+        }
+        return best;
+    };
+    if (!backward || dtype == PURINE_BF16) {
+        const HeldPlan few = widest(true);
+        if (few.width * bytes >= 48) return few;
     }
-    return best;
+    return widest(false);
 }
 
 template <typename F>
@@ -613,7 +623,8 @@ hipError_t by_vector(int dtype, int v, F&& f) {
 // f(pieces as a constant, threads as a constant)
 template <int MOST, typename F>
 hipError_t by_pieces(const HeldPlan& h, F&& f) {
-    if (h.threads == 256) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 256>());
+    if (h.threads == 256 && h.pieces <= 4) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 256>());
+    if (h.threads == 256) return f(std::integral_constant<int, HELD_GRAD>(), std::integral_constant<int, 256>());
     if (h.pieces <= 4) return f(std::integral_constant<int, 4>(), std::integral_constant<int, HT>());
     if (h.pieces <= HELD_GRAD) return f(std::integral_constant<int, HELD_GRAD>(), std::integral_constant<int, HT>());
     if constexpr (MOST > HELD_GRAD) return f(std::integral_constant<int, MOST>(), std::integral_constant<int, HT>());
