@@ -252,7 +252,8 @@ __device__ __forceinline__ void grad_of(float x, float dy, float mu, float rstd,
 }
 
 template <typename T, int V, int ACT>
-__global__ __launch_bounds__(NT) void norm_grad_sums_kernel(const NormParams p) {
+__global__ __launch_bounds__(NT, 4) void norm_grad_sums_kernel(const NormParams p) {
+    constexpr int BATCH = V == 8 && ACT == PURINE_ACT_GELU ? 3 : AHEAD;        // (of what 128 registers hold)
     const Place<V> at(p);
     float s[V], q[V];
 #pragma unroll
@@ -266,16 +267,23 @@ __global__ __launch_bounds__(NT) void norm_grad_sums_kernel(const NormParams p) 
         }
         const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
         const T* dy = (const T*)p.dy + at.n * p.dy_ns + at.c;
-        for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
-            Pack<T, V> in[AHEAD], gr[AHEAD];
+        // (a batch of positions ahead of its use: 64 x 12544 x 64 in bf16 43.8 us, without 53.6; its 206 MB at the rate of a copy 40)
+        Pack<T, V> in[BATCH], gr[BATCH], in_next[BATCH], gr_next[BATCH];
+        auto load = [&](int t) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
+            for (int u = 0; u < BATCH; ++u) {
                 const int64_t row = (int64_t)min(t + u * at.R, at.s1 - 1) * p.C;
-                in[u] = *reinterpret_cast<const Pack<T, V>*>(x + row);
-                gr[u] = *reinterpret_cast<const Pack<T, V>*>(dy + row);
+                in_next[u] = *reinterpret_cast<const Pack<T, V>*>(x + row);
+                gr_next[u] = *reinterpret_cast<const Pack<T, V>*>(dy + row);
             }
+        };
+        load(at.s0 + at.r);
+        for (int t = at.s0 + at.r; t < at.s1; t += BATCH * at.R) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
+            for (int u = 0; u < BATCH; ++u) { in[u] = in_next[u]; gr[u] = gr_next[u]; }
+            load(t + BATCH * at.R);
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
                 if (t + u * at.R >= at.s1) break;
                 float v[V], d[V];
                 widen_v<T, V>(in[u], v);
