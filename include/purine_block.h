@@ -31,7 +31,7 @@ typedef enum {
  * (whole 16-byte packets). scale, shift: F32 of C elements, or NULL (ones, zeros). mean, rstd: F32 [N, groups], both or neither:
  * the gradient needs them. y may be x itself. Sums are fp32, taken about a value of the channel, so that a large mean
  * does not cost the variance its digits. eps > 0.
- * ws: purine_group_norm_workspace_bytes(0, ...). */
+ * ws: purine_group_norm_workspace_bytes(0, ...), one answer for whichever kernels a call gets. */
 size_t purine_group_norm_workspace_bytes(int backward, const int64_t x_dim[4], int ndim, int groups, int32_t dtype);
 int purine_group_norm_fwd(const purine_tensor* x, const purine_tensor* scale, const purine_tensor* shift, purine_tensor* y,
                           purine_tensor* mean, purine_tensor* rstd, int groups, float eps, int act, void* ws,
@@ -49,8 +49,8 @@ int purine_group_norm_bwd(const purine_tensor* x, const purine_tensor* scale, co
  * b and r may be NULL. pre [N, K] (or NULL) receives x w^T + b, which the gradient needs. Matrices may set nstride, the
  * distance between rows (whole 16-byte packets): columns of wider buffers. y may be r itself. Sums are fp32; every result
  * is rounded once.
- * F32: three exact bf16 parts per operand and six products, as for convolutions (purine.h); operands from 2^-100 in magnitude
- * keep all their bits. Results that are infinite or NaN are computed again as plain fp32 sums.
+ * F32: three exact bf16 parts per operand and six products, as for convolutions (purine.h, "F32 arithmetic"); results that are infinite
+ * or NaN are computed again as plain fp32 sums. Up to four rows of whole 16-byte packets: fp32 products.
  * pass for the workspace query: PURINE_CONV_FWD, _BWD_DATA, _BWD_WEIGHT. */
 size_t purine_linear_workspace_bytes(int pass, int64_t N, int64_t C, int64_t K, int32_t dtype);
 int purine_linear_fwd(const purine_tensor* x, const purine_tensor* w, const purine_tensor* b, const purine_tensor* r,

@@ -3,7 +3,8 @@
 //     g = grad_scale dw;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
 //     w = w (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
 //
-// Bound: HBM, every tensor read once and written once. The table of tensors travels in the kernel arguments, 40 tensors a launch,
+// Bound: HBM, every tensor read once and written once: 62 M parameters (AlexNet) with fp32 states 342 us (28 bytes a parameter, 5.1 TB/s), with bf16 gradients, a
+// bf16 copy and 8-bit states 195 us (16 bytes, 5.1 TB/s); 12 tensors of 164 k parameters in all 4.8 us, a launch. The table of tensors travels in the kernel arguments, 40 tensors a launch,
 // so that a step needs no memory of its own; a workgroup takes 2048 consecutive elements of one tensor, found from the tensors' first
 // workgroups in the table.
 #include <math.h>

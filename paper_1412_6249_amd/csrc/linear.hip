@@ -182,8 +182,9 @@ size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 size_t packed_bytes(int64_t rows, int64_t K, bool in, int planes) { return whole((size_t)(in ? rows * packed_ld(K) : K * packed_ld(rows)) * 2 * planes); }
 bool whole_packets(int64_t rows, int64_t K, bool in) { return (in ? K : rows) % 8 == 0; }
 
-// g = dy act'(pre), and the sums of its columns over a slice of the rows. Bound: HBM. A thread owns V neighbouring columns (16 bytes where
-// rows are whole packets) and walks down the slice, two rows ahead of their use; the threads of a column join in LDS, the slices in a
+// g = dy act'(pre), and the sums of its columns over a slice of the rows. Bound: HBM (us: 8192 x 8192 bf16 85, 403 MB at 4.7 TB/s; 100352 x 96 12.3,
+// 58 MB at 4.7; 777 x 333 fp32 in single elements 4.4), then a launch of 4 - 5 for the slices' sums. A thread owns V neighbouring columns (16 bytes where
+// rows are whole packets) and walks down the slice, four rows at a time; the threads of a column join in LDS, the slices in a
 // second kernel, both in order.
 struct ActParams {
     const void* pre; const void* dy; void* g; float* part;

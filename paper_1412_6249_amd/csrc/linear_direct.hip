@@ -3,13 +3,14 @@
 //     out[i][j] = epilogue(sum over k of A(i, k) B(j, k))
 //
 // Up to four rows (linear_row_kernel): a wavefront reads 1024 bytes of a row of B at a time, four such rows beside each other, multiplies them with the same
-// part of the rows of A in fp32, and adds up its lanes; four wavefronts share the reduction. Bound: reading B.
+// part of the rows of A in fp32, and adds up its lanes; four wavefronts share the reduction. Bound: reading B (1 x 4096 x 4096 bf16: 33.6 MB in 7.2 us from memory,
+// 4.6 from the caches).
 //
 // Else (linear_direct_kernel) a workgroup owns 16 TI x 16 TJ results. Its wavefronts take the steps of the reduction (32 elements) in turn, load their fragments straight from
 // memory, a group of steps ahead, multiply them (bf16 as they are; fp32 as three exact bf16 parts, the five small products in an accumulator of
 // their own) and add their sums through LDS in order. Nothing is laid out beforehand and there is no second launch.
 //
-// Bound: a chain of a few loads, and one launch.
+// Bound: a chain of a few loads, and one launch (777 x 501 x 333 fp32: each pass 10 - 13 us; packed operands, product and join of linear.hip take 24 - 26).
 #include "linear_gemm.h"
 #include "linear_finish.h"
 #include "packets.h"
