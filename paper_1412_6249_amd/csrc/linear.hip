@@ -61,44 +61,41 @@ __global__ __launch_bounds__(256) void linear_pack_kernel(const T* __restrict__ 
     }
 }
 
-// Adds the partial sums of the splits in order and finishes the results. A thread has V neighbouring columns of a row, and `lanes`
-// threads share the splits of one (few results of many splits: dw of a narrow layer over many positions). SPLIT3: sums of an fp32 product's parts.
+// Adds the partial sums of the splits in order and finishes the results. A thread has four neighbouring columns of a row of the sums, which are padded to whole
+// 16-byte packets, and `lanes` threads share the splits of one (few results of many splits: dw of a narrow layer over many positions). SPLIT3: sums of an
+// fp32 product's parts. Bound: memory (14173 x 4771 fp32, 541 MB: 147 us, rows that are no whole packets are stored element by element; with sums in such rows, one result a
+// thread, 252, and the product before it 305 for 169).
 struct JoinParams { const float* part; Finish f; Source a, b; int rows, cols, K, splits, lanes; };
-template <typename E, typename O, int V>
+template <typename E, typename O>
 __global__ __launch_bounds__(256) void linear_join_kernel(const JoinParams p) {
     constexpr bool SPLIT3 = sizeof(E) == 4;
-    __shared__ float sums[256][V + 1];
+    __shared__ float sums[256][5];
     const int lanes = p.lanes, per = 256 / lanes, lane = threadIdx.x / per, mine = threadIdx.x % per;
-    const int64_t chunks = p.cols / V, total = p.rows * chunks, t = (int64_t)blockIdx.x * per + mine, all = (int64_t)p.rows * p.cols;
-    float v[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = 0.0f;
+    const unsigned chunks = (unsigned)(p.cols + 3) / 4, total = (unsigned)p.rows * chunks, t = blockIdx.x * (unsigned)per + mine;     // (below 2^31)
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (t < total) {
         const int each = (p.splits + lanes - 1) / lanes, last = min(p.splits, (lane + 1) * each);
-        const float* src = p.part + t * V;
+        const float4* src = reinterpret_cast<const float4*>(p.part) + t;
 #pragma unroll 4
         for (int s = lane * each; s < last; ++s) {
-            if constexpr (V == 4) {
-                const float4 x = *reinterpret_cast<const float4*>(src + s * all);
-                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-            } else {
-                v[0] += src[s * all];
-            }
+            const float4 x = src[(int64_t)s * total];
+            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
         }
     }
     if (lanes > 1) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) sums[threadIdx.x][e] = v[e];
+        for (int e = 0; e < 4; ++e) sums[threadIdx.x][e] = v[e];
         __syncthreads();
         if (lane) return;
         for (int l = 1; l < lanes; ++l)
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] += sums[threadIdx.x + l * per][e];
+            for (int e = 0; e < 4; ++e) v[e] += sums[threadIdx.x + l * per][e];
     }
     if (t >= total) return;
-    const int i = (int)(t / chunks), j = (int)(t - i * chunks) * V;
+    const int i = (int)(t / chunks), j = (int)(t - i * chunks) * 4;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
+    for (int e = 0; e < 4; ++e) {
+        if (j + e >= p.cols) break;
         float z = v[e];
         if constexpr (SPLIT3) z = joined(z, p.a, p.b, i, j + e, p.K);
         finish<E, O>(p.f, i, j + e, z);
@@ -176,6 +173,8 @@ DirectForm direct_form(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_
     return form;
 }
 
+// rows of partial sums: whole 16-byte packets
+int64_t part_ld(int64_t cols) { return (cols + 3) / 4 * 4; }
 int64_t packed_ld(int64_t len) { return (len + 7) / 8 * 8; }
 size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 // bytes of an operand's copy: reduction inner (rows x K) or outer (K x rows)
@@ -287,7 +286,7 @@ size_t linear_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_
     size_t n = 0;
     if (planes == 3 || !whole_packets(rows, K, a_in)) n += packed_bytes(rows, K, a_in, planes);
     if (planes == 3 || !whole_packets(cols, K, b_in)) n += packed_bytes(cols, K, b_in, planes);
-    if (planes == 3 || g.splits > 1) n += (size_t)g.splits * rows * cols * 4;
+    if (planes == 3 || g.splits > 1) n += (size_t)g.splits * rows * part_ld(cols) * 4;
     return n;
 }
 
@@ -296,13 +295,11 @@ namespace {
 template <typename E, typename O>
 hipError_t join(const JoinParams& q, hipStream_t st) {
     JoinParams p = q;
-    const bool v4 = p.cols % 4 == 0;
-    const int64_t threads = (int64_t)p.rows * p.cols / (v4 ? 4 : 1);
+    const int64_t threads = (int64_t)p.rows * part_ld(p.cols) / 4;
     p.lanes = 1;
     while (p.lanes < 32 && p.lanes * 4 <= p.splits && threads * p.lanes < 256 * 512) p.lanes *= 2;
     const int64_t per = 256 / p.lanes, grid = (threads + per - 1) / per;
-    if (v4) hipLaunchKernelGGL((linear_join_kernel<E, O, 4>), dim3((unsigned)grid), dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((linear_join_kernel<E, O, 1>), dim3((unsigned)grid), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((linear_join_kernel<E, O>), dim3((unsigned)grid), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 
@@ -363,6 +360,7 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
     p.group = 8;
     const bool second = g.splits > 1 || f32;
     p.part = (float*)scratch;
+    p.part_ld = (int)part_ld(c.cols);
     p.out = c.out; p.out_ld = c.out_ld; p.out_f32 = c.out_dtype == PURINE_F32;
     p.bias = c.bias; p.res = c.res; p.res_ld = c.res_ld; p.pre = c.pre; p.pre_ld = c.pre_ld; p.slope = c.slope; p.slope_ld = c.slope_ld;
     p.accumulate = c.accumulate;

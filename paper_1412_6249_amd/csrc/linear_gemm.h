@@ -47,7 +47,8 @@ struct GemmParams {
     int steps, per_split, splits;
     int planes;                            // 1, or 3: fp32 operands in three bf16 parts
     int tiles_i, tiles_j, group;           // group: row tiles that share their columns' panels in L2
-    float* part;                           // [split][rows][cols]
+    float* part;                           // [split][rows][part_ld]: rows of whole 16-byte packets
+    int part_ld;
     void* out; const void* bias; const void* res; void* pre; const void* slope;
     int64_t out_ld, res_ld, pre_ld, slope_ld;
     int out_f32, accumulate;
@@ -514,14 +515,14 @@ __global__ __launch_bounds__(256, BI * BUFS > 256 ? 1 : BI * BUFS > 128 ? 2 : 4)
                 }
             }
         } else {
-            const bool whole = n >= 8 && (EPI == PART ? p.cols % 4 == 0 : p.vectors);
+            const bool whole = n >= 8 && (EPI == PART || p.vectors);
 #pragma unroll 1
             for (int it = 0; it < ITEMS; ++it) {
                 float v[8], t[8], pre[8];
                 const int row = item(it, v);
                 if (row >= p.rows || n <= 0) continue;
                 if constexpr (EPI == PART) {
-                    put8(p.part + ((int64_t)split * p.rows + row) * p.cols + col, whole, n, v);
+                    put8(p.part + ((int64_t)split * p.rows + row) * p.part_ld + col, whole, n, v);
                 } else {
                     if (reads) get8(other + row * other_ld + col, whole, n, t);
                     combine(v, t, pre);
