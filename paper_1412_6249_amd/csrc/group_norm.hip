@@ -76,6 +76,7 @@ struct NormParams {
     int64_t x_ns, dy_ns, out_ns;
     const float* scale; const float* shift;     // or null
     float2* part;              // per image, slice and channel: the two sums
+    float* about;              // per image and channel: the value that x's sums are taken about
     const float* mean; const float* rstd;       // gradient: as saved
     float* mean_out; float* rstd_out;           // or null
     float* dscale; float* dshift;               // or null
@@ -186,6 +187,9 @@ __global__ __launch_bounds__(NT) void norm_sums_kernel(const NormParams p) {
     float2* o = p.part + ((int64_t)at.n * p.slices + at.slice) * p.C + at.c;
 #pragma unroll
     for (int i = 0; i < V; ++i) o[i] = make_float2(s[i], q[i]);
+    if (at.slice == 0)
+#pragma unroll
+        for (int i = 0; i < V; ++i) p.about[(int64_t)at.n * p.C + at.c + i] = k[i];
 }
 
 // The sums of a channel over the slices, in order.
@@ -201,19 +205,17 @@ __device__ __forceinline__ float2 over_slices(const NormParams& p, int n, int c)
 __device__ __forceinline__ float scale_of(const NormParams& p, int c) { return p.scale ? p.scale[c] : 1.0f; }
 __device__ __forceinline__ float shift_of(const NormParams& p, int c) { return p.shift ? p.shift[c] : 0.0f; }
 
+// (y may be x: a workgroup reads no element of x but those that it replaces, the values that the sums are about come from the scratch)
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(NT) void norm_apply_kernel(const NormParams p) {
     __shared__ float2 stat[NT * V + 1];
     const Place<V> at(p);
-    const T* x0 = (const T*)p.x + at.n * p.x_ns;
     const int g0 = at.c0 / p.per, g1 = (at.c1 - 1) / p.per;
     for_groups<NT>(g1 - g0 + 1, p.per, [&](int g, int lane, int lanes, auto&& sum) {
         const int first = (g0 + g) * p.per;
         const float2 o = group_stats(p, lane, lanes, sum, [&](int c, float& s, float& q, float& k) {
             const float2 w = over_slices(p, at.n, first + c);
-            float v[1];
-            load_v<T, 1>(x0 + first + c, v);
-            s = w.x; q = w.y; k = v[0];
+            s = w.x; q = w.y; k = p.about[(int64_t)at.n * p.C + first + c];
         });
         if (lane == 0) {
             stat[g] = o;
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(NT) void norm_apply_kernel(const NormParams p) {
         const float2 o = stat[(at.c + i) / p.per - g0];
         mu[i] = o.x; a[i] = o.y * scale_of(p, at.c + i); b[i] = shift_of(p, at.c + i);
     }
-    const T* x = x0 + at.c;
+    const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
     T* y = (T*)p.out + at.n * p.out_ns + at.c;
     for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
         Pack<T, V> in[AHEAD];
@@ -650,6 +652,7 @@ NormParams params_of(const NormShape& s, void* ws) {
     p.rows = (s.S + p.slices - 1) / p.slices;
     p.slices = (s.S + p.rows - 1) / p.rows;
     p.part = (float2*)ws;
+    p.about = (float*)(p.part + (int64_t)s.N * p.slices * s.C);
     return p;
 }
 
@@ -668,7 +671,7 @@ unsigned held_grid(NormParams& p, const HeldPlan& h) {
 }  // namespace
 
 // What the sliced kernels take, whichever a call gets (the held ones need a slice's at most).
-size_t group_norm_ws_bytes(int64_t N, int64_t S, int64_t C) { return (size_t)(N * slices_of(N, S, C) * C) * sizeof(float2); }
+size_t group_norm_ws_bytes(int64_t N, int64_t S, int64_t C) { return (size_t)(N * slices_of(N, S, C) * C) * sizeof(float2) + (size_t)(N * C) * sizeof(float); }
 
 hipError_t launch_group_norm_fwd(int dtype, const NormShape& s, const void* x, const float* scale, const float* shift, void* y, float* mean,
                                  float* rstd, void* ws, hipStream_t st) {
