@@ -29,8 +29,8 @@ typedef enum {
  * with mean and (biased) variance over the group's channels and all positions. groups = 1 normalises a whole image,
  * groups = C every channel by itself. x and y share one dtype (F32 or BF16) and extents; 4-axis x, y, dy, dx may set nstride
  * (whole 16-byte packets). scale, shift: F32 of C elements, or NULL (ones, zeros). mean, rstd: F32 [N, groups], both or neither:
- * the gradient needs them. y may be x itself. Sums are fp32, taken about a value of the channel, so that a large mean
- * does not cost the variance its digits. eps > 0.
+ * the gradient needs them. y may be x itself. Sums are fp32; the variance is joined from squares about
+ * means, so that neither a large mean nor first positions unlike the others cost it digits. eps > 0.
  * ws: purine_group_norm_workspace_bytes(0, ...), one answer for whichever kernels a call gets. */
 size_t purine_group_norm_workspace_bytes(int backward, const int64_t x_dim[4], int ndim, int groups, int32_t dtype);
 int purine_group_norm_fwd(const purine_tensor* x, const purine_tensor* scale, const purine_tensor* shift, purine_tensor* y,

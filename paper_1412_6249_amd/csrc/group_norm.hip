@@ -4,9 +4,11 @@
 //     dz = dy act'(z),  h = dz scale,  dx = rstd (h - avg(h) - xhat avg(h xhat)),  dshift = sum dz,  dscale = sum dz xhat
 //
 // A thread owns V neighbouring channels (16 bytes where the row allows it) and walks down the positions, so that loads are whole pieces of
-// rows and the affine parameters stay in registers. Sums are kept per channel, which serves any number of channels per group: for
-// the statistics s = sum (x - k), q = sum (x - k)^2 about the channel's value k at the image's first position (a large mean
-// costs no digits), for the gradient sum dz and sum dz xhat. They are joined in a fixed order.
+// rows and the affine parameters stay in registers. Sums are kept per channel, which serves any number of channels per group. For the statistics they are
+// means and sums of squares about these means: of a few positions of a thread about one of them, then of more and more of them by
+//     n = a + b,  mean = (a mean_a + b mean_b) / n,  M = M_a + a (mean_a - mean)^2 + M_b + b (mean_b - mean)^2,
+// so that no difference of large sums is taken, whatever values come first (means are kept relative to the channel's value k at the image's first position:
+// of a large common mean no digits are lost). For the gradient they are sum dz and sum dz xhat. Everything is joined in a fixed order.
 //
 // Bound: HBM, and with an activation the vector units nearly as much (about 30 instructions a gradient element). us, bf16: 128 x 784 x 192 in 32 groups, SiLU, held:
 // forward 20 (77 MB; 15 at the rate of a copy), gradient 34 (115 MB; 23); 64 x 12544 x 64 in 32 groups, GELU by tanh, sliced: sums 20 and result 38 (103 and 206 MB;
@@ -75,8 +77,8 @@ struct NormParams {
     const void* x; const void* dy; void* out;
     int64_t x_ns, dy_ns, out_ns;
     const float* scale; const float* shift;     // or null
-    float2* part;              // per image, slice and channel: the two sums
-    float* about;              // per image and channel: the value that x's sums are taken about
+    float2* part;              // per image, slice and channel: mean and sum of squares about it, or the gradient's two sums
+    float* about;              // per image and channel: the value that the means are relative to
     const float* mean; const float* rstd;       // gradient: as saved
     float* mean_out; float* rstd_out;           // or null
     float* dscale; float* dshift;               // or null
@@ -101,19 +103,57 @@ __device__ __forceinline__ void for_groups(int count, int per, F&& f) {
     for (int g = threadIdx.x / lanes; g < count; g += THREADS / lanes) f(g, (int)threadIdx.x & (lanes - 1), lanes, sum);
 }
 
-// Mean and rstd of a group from its channels' sums: channel(c, s, q, k) gives those of the group's c-th channel.
-template <typename Sum, typename Channel>
-__device__ __forceinline__ float2 group_stats(const NormParams& p, int lane, int lanes, Sum&& sum, Channel&& channel) {
-    const float n = (float)p.S;
-    float all = 0.0f, s, q, k;
-    for (int c = lane; c < p.per; c += lanes) { channel(c, s, q, k); all += k + s / n; }
-    const float mu = sum(all) / (float)p.per;
-    float var = 0.0f;
-    for (int c = lane; c < p.per; c += lanes) {
-        channel(c, s, q, k);
-        const float d = s / n, off = k + d - mu;
-        var += (fmaxf(q - s * d, 0.0f) + 0.0f * q) / n + off * off;      // (not below zero; infinities stay NaN)
+// Joins the means of `width` channels, and the sums of squares about them, over R rows of threads: sums[r * width + c] is of the positions r, r + R, ... of
+// `total`. All threads take part; the result is in the first row. Sixteen rows at a time, so that a few rounds do and the loads of a round wait together;
+// about the first one's mean, which loses sixteen times the last place at most, whatever it is.
+template <int THREADS>
+__device__ __forceinline__ void join_moments(float2* sums, int width, int R, int total) {
+    constexpr int STEP = 16, AT_ONCE = 8;                           // (all sixteen at once would take the registers of a wavefront)
+    const int columns = min(width, THREADS), lanes = THREADS / columns, c0 = threadIdx.x % columns, l = threadIdx.x / columns;
+    const int base = total / R;                                     // positions of a row: base, or one more in the first `more`
+    const float each = (float)base, more = (float)(total - base * R), most = (float)R;
+    __syncthreads();
+    for (int rows = R, span = 1; rows > 1; rows = (rows + STEP - 1) / STEP, span *= STEP) {
+        const int next = (rows + STEP - 1) / STEP;
+        const float wide = (float)span;
+        for (int c1 = 0; c1 < width; c1 += columns)
+            for (int j1 = 0; j1 < next; j1 += lanes) {
+                const int c = c1 + c0, j = j1 + l, first = j * STEP, end = min(first + STEP, rows);
+                const bool mine = c < width && j < next && l < lanes;
+                float2 o = make_float2(0.0f, 0.0f);
+                if (mine) {
+                    const float about = sums[first * width + c].x;
+                    float a = 0.0f, b = 0.0f, n = 0.0f, row = (float)first * wide;
+#pragma unroll 1
+                    for (int u0 = first; u0 < end; u0 += AT_ONCE) {
+                        float2 v[AT_ONCE];
+#pragma unroll
+                        for (int u = 0; u < AT_ONCE; ++u) v[u] = sums[min(u0 + u, rows - 1) * width + c];
+#pragma unroll
+                        for (int u = 0; u < AT_ONCE; ++u, row += wide) {
+                            const float w = fmaxf(each * fminf(wide, most - row) + __builtin_amdgcn_fmed3f(more - row, 0.0f, wide), 0.0f), d = v[u].x - about;
+                            n += w;
+                            a += w * d;
+                            b += w * (d * d) + (u0 + u < rows ? v[u].y : 0.0f);
+                        }
+                    }
+                    const float d = a * __builtin_amdgcn_rcpf(fmaxf(n, 1.0f));
+                    o = make_float2(about + d, b - a * d);
+                }
+                __syncthreads();                   // (rows that others read: what is written lies before what is still to be read)
+                if (mine) sums[j * width + c] = o;
+            }
+        __syncthreads();
     }
+}
+
+// Mean and rstd of a group: mean(c) gives its c-th channel's mean, squares(c, mu) that channel's sum of squares about mu.
+template <typename Sum, typename Mean, typename Squares>
+__device__ __forceinline__ float2 group_stats(const NormParams& p, int lane, int lanes, Sum&& sum, Mean&& mean, Squares&& squares) {
+    float all = 0.0f, var = 0.0f;
+    for (int c = lane; c < p.per; c += lanes) all += mean(c);
+    const float mu = sum(all) / (float)p.per;
+    for (int c = lane; c < p.per; c += lanes) var += squares(c, mu) / (float)p.S;
     var = sum(var) / (float)p.per;
     return make_float2(mu, 1.0f / sqrtf(var + p.eps));
 }
@@ -162,36 +202,79 @@ constexpr int AHEAD = 4;                       // positions that a thread loads 
 
 template <typename T, int V>
 __global__ __launch_bounds__(NT) void norm_sums_kernel(const NormParams p) {
+    __shared__ float2 sums[NT * V];
     const Place<V> at(p);
     const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
-    float k[V], s[V], q[V];
+    float k[V], mean[V], m2[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i] = q[i] = k[i] = 0.0f;
+    for (int i = 0; i < V; ++i) mean[i] = m2[i] = k[i] = 0.0f;
     if (at.on) {
         load_v<T, V>(x, k);
+        Pack<T, V> in[AHEAD], next[AHEAD];
+        auto load = [&](int t) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) next[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(t + u * at.R, at.s1 - 1) * p.C);
+        };
+        float before = 0.0f;
+        load(at.s0 + at.r);
         for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
-            Pack<T, V> in[AHEAD];
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) in[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(t + u * at.R, at.s1 - 1) * p.C);
+            for (int u = 0; u < AHEAD; ++u) in[u] = next[u];
+            load(t + AHEAD * at.R);
+            float first[V], s[V], q[V], count = 1.0f;
+            widen_v<T, V>(in[0], first);
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
+            for (int i = 0; i < V; ++i) s[i] = q[i] = 0.0f;
+#pragma unroll
+            for (int u = 1; u < AHEAD; ++u) {
                 if (t + u * at.R >= at.s1) break;
                 float v[V];
                 widen_v<T, V>(in[u], v);
 #pragma unroll
-                for (int i = 0; i < V; ++i) { const float d = v[i] - k[i]; s[i] += d; q[i] += d * d; }
+                for (int i = 0; i < V; ++i) { const float d = v[i] - first[i]; s[i] += d; q[i] += d * d; }
+                count += 1.0f;
             }
+            const float inv = __builtin_amdgcn_rcpf(count), share = count * __builtin_amdgcn_rcpf(before + count), cross = before * share;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = s[i] * inv, off = (first[i] - k[i]) + d - mean[i];
+                mean[i] += off * share;
+                m2[i] += (q[i] - s[i] * d) + cross * (off * off);
+            }
+            before += count;
         }
+#pragma unroll
+        for (int i = 0; i < V; ++i) sums[threadIdx.x * V + i] = make_float2(mean[i], m2[i]);
     }
-    if (!join_rows<V>(at, s, q)) return;
+    join_moments<NT>(sums, at.tile * V, at.R, at.s1 - at.s0);
+    if (at.r != 0) return;
     float2* o = p.part + ((int64_t)at.n * p.slices + at.slice) * p.C + at.c;
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = make_float2(s[i], q[i]);
+    for (int i = 0; i < V; ++i) o[i] = sums[threadIdx.x * V + i];
     if (at.slice == 0)
 #pragma unroll
         for (int i = 0; i < V; ++i) p.about[(int64_t)at.n * p.C + at.c + i] = k[i];
 }
 
+// f(0) + ... + f(n - 1) as eight sums: a thousand terms one after the other would lose ten times the last place.
+template <typename F>
+__device__ __forceinline__ float sum_of(int n, F&& f) {
+    float s[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s[u] = 0.0f;
+    int k = 0;
+    for (; k + 8 <= n; k += 8)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s[u] += f(k + u);
+    if (k < n) {
+        float v[7];
+#pragma unroll
+        for (int u = 0; u < 7; ++u) v[u] = f(min(k + u, n - 1));
+#pragma unroll
+        for (int u = 0; u < 7; ++u) s[u] += k + u < n ? v[u] : 0.0f;
+    }
+    return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+}
 // The sums of a channel over the slices, in order.
 __device__ __forceinline__ float2 over_slices(const NormParams& p, int n, int c) {
     const float2* part = p.part + (int64_t)n * p.slices * p.C + c;
@@ -213,10 +296,21 @@ __global__ __launch_bounds__(NT) void norm_apply_kernel(const NormParams p) {
     const int g0 = at.c0 / p.per, g1 = (at.c1 - 1) / p.per;
     for_groups<NT>(g1 - g0 + 1, p.per, [&](int g, int lane, int lanes, auto&& sum) {
         const int first = (g0 + g) * p.per;
-        const float2 o = group_stats(p, lane, lanes, sum, [&](int c, float& s, float& q, float& k) {
-            const float2 w = over_slices(p, at.n, first + c);
-            s = w.x; q = w.y; k = p.about[(int64_t)at.n * p.C + first + c];
-        });
+        const float* about = p.about + (int64_t)at.n * p.C + first;
+        const float2* part = p.part + (int64_t)at.n * p.slices * p.C + first;
+        const int last = p.slices - 1;
+        const float n = (float)p.rows, n_last = (float)(p.S - last * p.rows);
+        const float2 o = group_stats(
+            p, lane, lanes, sum,
+            [&](int c) {
+                const float s = sum_of(last, [&](int s) { return part[(int64_t)s * p.C + c].x; });
+                return about[c] + (n * s + n_last * part[(int64_t)last * p.C + c].x) / (float)p.S;
+            },
+            [&](int c, float mu) {
+                const float k = about[c] - mu;
+                auto squares = [k](float2 o, float n) { return o.y + n * ((k + o.x) * (k + o.x)); };
+                return sum_of(last, [&](int s) { return squares(part[(int64_t)s * p.C + c], n); }) + squares(part[(int64_t)last * p.C + c], n_last);
+            });
         if (lane == 0) {
             stat[g] = o;
             if (at.slice == 0 && p.mean_out) { p.mean_out[at.n * p.G + g0 + g] = o.x; p.rstd_out[at.n * p.G + g0 + g] = o.y; }
@@ -423,38 +517,52 @@ __device__ __forceinline__ void join_held(const float (&s)[V], const float (&q)[
 
 template <typename T, int V, int ACT, int NV, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_held_kernel(const NormParams p) {
-    __shared__ float2 sums[THREADS * V], chan[THREADS], stat[THREADS];
-    __shared__ float about[THREADS];           // the channels' values that the sums are taken about
+    __shared__ float2 sums[THREADS * V], stat[THREADS];
+    __shared__ float about[THREADS];           // the channels' values that the means are relative to
     const int b = held_block(), n = b / p.tiles, c0 = (b - n * p.tiles) * p.width, cv = p.width / V, R = THREADS / cv;
     const int r = threadIdx.x / cv, c = c0 + (int)threadIdx.x % cv * V;
     const bool on = r < R;
     const T* x = (const T*)p.x + n * p.x_ns + c;
     Pack<T, V> in[NV];
-    float k[V], s[V], q[V];
+    float k[V], mean[V], q[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i] = q[i] = k[i] = 0.0f;
+    for (int i = 0; i < V; ++i) mean[i] = q[i] = k[i] = 0.0f;
     if (on) {
         load_v<T, V>(x, k);
 #pragma unroll
         for (int u = 0; u < NV; ++u) in[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(r + u * R, p.S - 1) * p.C);
+        float s[V], first[V], count = 1.0f;
+        widen_v<T, V>(in[0], first);
 #pragma unroll
-        for (int u = 0; u < NV; ++u) {
+        for (int i = 0; i < V; ++i) s[i] = 0.0f;
+#pragma unroll
+        for (int u = 1; u < NV; ++u) {
             if (r + u * R >= p.S) break;
             float v[V];
             widen_v<T, V>(in[u], v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) { const float d = v[i] - k[i]; s[i] += d; q[i] += d * d; }
+            for (int i = 0; i < V; ++i) { const float d = v[i] - first[i]; s[i] += d; q[i] += d * d; }
+            count += 1.0f;
         }
+        const float inv = __builtin_amdgcn_rcpf(count);
+#pragma unroll
+        for (int i = 0; i < V; ++i) { const float d = s[i] * inv; mean[i] = (first[i] - k[i]) + d; q[i] -= s[i] * d; }
     }
     if (r == 0)
 #pragma unroll
         for (int i = 0; i < V; ++i) about[c - c0 + i] = k[i];
-    join_held<V, THREADS>(s, q, sums, chan, p.width, R, on);
+    if (on)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sums[threadIdx.x * V + i] = make_float2(mean[i], q[i]);
+    join_moments<THREADS>(sums, p.width, R, p.S);
     for_groups<THREADS>(p.width / p.per, p.per, [&](int g, int lane, int lanes, auto&& sum) {
-        const float2 o = group_stats(p, lane, lanes, sum, [&](int i, float& cs, float& cq, float& ck) {
-            const float2 w = chan[g * p.per + i];
-            cs = w.x; cq = w.y; ck = about[g * p.per + i];
-        });
+        const float2 o = group_stats(
+            p, lane, lanes, sum, [&](int i) { return about[g * p.per + i] + sums[g * p.per + i].x; },
+            [&](int i, float mu) {
+                const float2 w = sums[g * p.per + i];
+                const float off = about[g * p.per + i] - mu + w.x;
+                return w.y + (float)p.S * (off * off);
+            });
         if (lane == 0) {
             stat[g] = o;
             const int at = n * p.G + c0 / p.per + g;
