@@ -764,16 +764,37 @@ NormParams params_of(const NormShape& s, void* ws) {
     return p;
 }
 
-// Workgroups of the kernels that walk over positions (fewer than elements / 64, so fewer than 2^31).
-unsigned grid_of(NormParams& p, int v) {
+// Workgroups of an image in the kernels that walk over positions, and in the held ones.
+int64_t blocks_of(NormParams& p, int v) {
     p.tiles = (p.C / v + NT - 1) / NT;
-    return (unsigned)((int64_t)p.N * p.slices * p.tiles);
+    return (int64_t)p.slices * p.tiles;
 }
-unsigned held_grid(NormParams& p, const HeldPlan& h) {
+int64_t held_blocks(NormParams& p, const HeldPlan& h) {
     p.width = h.width;
     p.tiles = p.C / h.width;
     p.slices = 1;
-    return (unsigned)((int64_t)p.N * p.tiles);
+    return p.tiles;
+}
+// launch(parameters, workgroups) for all images, in as many calls as keep each below 2^31 threads (a launch ends at 2^32 of them: 2^24 images of a
+// workgroup each; an image has fewer).
+template <typename T, typename F>
+hipError_t over_images(const NormParams& p, int64_t blocks, int threads, F&& launch) {
+    const int64_t most = (((int64_t)1 << 31) / threads) / blocks, images = most < 1 ? 1 : most;
+    for (int64_t n = 0; n < p.N; n += images) {
+        NormParams q = p;
+        const int64_t groups = n * p.G;
+        q.N = (int)(p.N - n < images ? p.N - n : images);
+        q.x = (const T*)p.x + n * p.x_ns;
+        q.out = (T*)p.out + n * p.out_ns;
+        if (p.dy) q.dy = (const T*)p.dy + n * p.dy_ns;
+        if (p.mean) { q.mean += groups; q.rstd += groups; }
+        if (p.mean_out) { q.mean_out += groups; q.rstd_out += groups; }
+        q.part += n * p.slices * p.C;
+        q.about += n * p.C;
+        const hipError_t e = launch(q, dim3((unsigned)(q.N * blocks)));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
@@ -793,18 +814,21 @@ hipError_t launch_group_norm_fwd(int dtype, const NormShape& s, const void* x, c
         typedef decltype(t) T;
         return by_act(s.act, [&](auto A) {
             if (h.width) {
-                const unsigned grid = held_grid(p, h);
+                const int64_t blocks = held_blocks(p, h);
                 ProbeScope probe(st);
                 return by_pieces<HELD>(h, [&](auto P, auto H) {
-                    hipLaunchKernelGGL((norm_held_kernel<T, V.value, A.value, P.value, H.value>), dim3(grid), dim3(H.value), 0, st, p);
-                    return hipGetLastError();
+                    return over_images<T>(p, blocks, H.value, [&](const NormParams& q, dim3 grid) {
+                        hipLaunchKernelGGL((norm_held_kernel<T, V.value, A.value, P.value, H.value>), grid, dim3(H.value), 0, st, q);
+                        return hipGetLastError();
+                    });
                 });
             }
-            const unsigned grid = grid_of(p, v);
-            hipLaunchKernelGGL((norm_sums_kernel<T, V.value>), dim3(grid), dim3(NT), 0, st, p);
-            ProbeScope probe(st);
-            hipLaunchKernelGGL((norm_apply_kernel<T, V.value, A.value>), dim3(grid), dim3(NT), 0, st, p);
-            return hipGetLastError();
+            return over_images<T>(p, blocks_of(p, v), NT, [&](const NormParams& q, dim3 grid) {
+                hipLaunchKernelGGL((norm_sums_kernel<T, V.value>), grid, dim3(NT), 0, st, q);
+                ProbeScope probe(st);
+                hipLaunchKernelGGL((norm_apply_kernel<T, V.value, A.value>), grid, dim3(NT), 0, st, q);
+                return hipGetLastError();
+            });
         });
     });
 }
@@ -822,18 +846,21 @@ hipError_t launch_group_norm_bwd(int dtype, const NormShape& s, const void* x, c
         typedef decltype(t) T;
         return by_act(s.act, [&](auto A) {
             if (h.width) {
-                const unsigned grid = held_grid(p, h);
+                const int64_t blocks = held_blocks(p, h);
                 ProbeScope probe(st);
                 return by_pieces<V.value == 8 ? HELD_GRAD : HELD>(h, [&](auto P, auto H) {
-                    hipLaunchKernelGGL((norm_grad_held_kernel<T, V.value, A.value, P.value, H.value>), dim3(grid), dim3(H.value), 0, st, p);
-                    return hipGetLastError();
+                    return over_images<T>(p, blocks, H.value, [&](const NormParams& q, dim3 grid) {
+                        hipLaunchKernelGGL((norm_grad_held_kernel<T, V.value, A.value, P.value, H.value>), grid, dim3(H.value), 0, st, q);
+                        return hipGetLastError();
+                    });
                 });
             }
-            const unsigned grid = grid_of(p, v);
-            hipLaunchKernelGGL((norm_grad_sums_kernel<T, V.value, A.value>), dim3(grid), dim3(NT), 0, st, p);
-            ProbeScope probe(st);
-            hipLaunchKernelGGL((norm_grad_apply_kernel<T, V.value, A.value>), dim3(grid), dim3(NT), 0, st, p);
-            return hipGetLastError();
+            return over_images<T>(p, blocks_of(p, v), NT, [&](const NormParams& q, dim3 grid) {
+                hipLaunchKernelGGL((norm_grad_sums_kernel<T, V.value, A.value>), grid, dim3(NT), 0, st, q);
+                ProbeScope probe(st);
+                hipLaunchKernelGGL((norm_grad_apply_kernel<T, V.value, A.value>), grid, dim3(NT), 0, st, q);
+                return hipGetLastError();
+            });
         });
     });
     if (e != hipSuccess || !dscale) return e;
