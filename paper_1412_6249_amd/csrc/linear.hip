@@ -238,13 +238,14 @@ __global__ __launch_bounds__(ANT) void act_bwd_kernel(const ActParams p) {
 #pragma unroll
     for (int e = 0; e < V; ++e) o[e] = sum[e];
 }
-// CS columns per workgroup, the slices over 256 / CS threads each.
+// CS columns per workgroup, the slices over 256 / CS threads each. first: the launch's first workgroup.
 template <typename O, int CS>
-__global__ __launch_bounds__(256) void column_sums_kernel(const float* part, O* db, int slices, int K, int accumulate) {
+__global__ __launch_bounds__(256) void column_sums_kernel(const float* part, O* db, int slices, int K, int accumulate, unsigned first) {
     __shared__ float sums[256 / CS][CS + 1];
-    const int l = threadIdx.x % CS, r = threadIdx.x / CS, j = blockIdx.x * CS + l;
+    const int l = threadIdx.x % CS, r = threadIdx.x / CS;
+    const unsigned j = (first + blockIdx.x) * CS + l;
     float sum = 0.0f;
-    if (j < K) {
+    if (j < (unsigned)K) {
 #pragma unroll 8
         for (int s = r; s < slices; s += 256 / CS) sum += part[(size_t)s * K + j];
     }
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const float* part, O* 
         if (r < half) sums[r][l] += sums[r + half][l];
         __syncthreads();
     }
-    if (r || j >= K) return;
+    if (r || j >= (unsigned)K) return;
     sum = sums[0][l];
     if (accumulate) sum += widen<O>(db[j]);
     narrow(sum, db + j);
@@ -263,8 +264,13 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const float* part, O* 
 // the line eight times (256 slices of 8192: 12.9 us by four, 5.0 by 32).
 template <typename O>
 hipError_t column_sums(const float* part, O* db, int slices, int K, int accumulate, hipStream_t st) {
-    if (K >= 4096) hipLaunchKernelGGL((column_sums_kernel<O, 32>), dim3((unsigned)((K + 31) / 32)), dim3(256), 0, st, part, db, slices, K, accumulate);
-    else hipLaunchKernelGGL((column_sums_kernel<O, 4>), dim3((unsigned)((K + 3) / 4)), dim3(256), 0, st, part, db, slices, K, accumulate);
+    if (K < 4096) hipLaunchKernelGGL((column_sums_kernel<O, 4>), dim3((unsigned)((K + 3) / 4)), dim3(256), 0, st, part, db, slices, K, accumulate, 0u);
+    else {
+        // (below 2^32 threads a launch)
+        const unsigned groups = ((unsigned)K + 31) / 32, most = 1u << 23;
+        for (unsigned from = 0; from < groups; from += most)
+            hipLaunchKernelGGL((column_sums_kernel<O, 32>), dim3(groups - from < most ? groups - from : most), dim3(256), 0, st, part, db, slices, K, accumulate, from);
+    }
     return hipGetLastError();
 }
 // Rows of a slice where threads own V columns: some 1024 workgroups, and one batch of loads per thread at least.
@@ -279,7 +285,9 @@ int act_rows(int64_t N, int64_t K, int V) {
 
 }  // namespace
 
-size_t linear_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_in, int dtype) {
+namespace {
+
+size_t piece_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_in, int dtype) {
     if (direct_form(rows, cols, K, a_in, b_in, dtype) != DIRECT_NONE) return 0;
     const int planes = dtype == PURINE_F32 ? 3 : 1;
     const GemmPlan g = plan_gemm(rows, cols, K, planes);
@@ -290,7 +298,33 @@ size_t linear_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_
     return n;
 }
 
-namespace {
+// Rows and columns of a launch at most: a launch ends at 2^32 threads, and the single row's kernel has 64 for a column.
+constexpr int64_t MOST = (int64_t)1 << 25;
+// The rows and columns [i, i + rows) x [j, j + cols) of a product.
+LinearCall part_of(const LinearCall& c, int64_t i, int64_t rows, int64_t j, int64_t cols) {
+    const int64_t es = c.dtype == PURINE_F32 ? 4 : 2, os = c.out_dtype == PURINE_F32 ? 4 : 2;
+    auto at = [](auto* p, int64_t bytes) { return p ? (decltype(p))((const char*)p + bytes) : p; };
+    LinearCall q = c;
+    q.rows = rows; q.cols = cols;
+    q.a = at(c.a, i * (c.a_in ? c.a_ld : 1) * es);
+    q.b = at(c.b, j * (c.b_in ? c.b_ld : 1) * es);
+    q.bias = at(c.bias, j * es);
+    q.res = at(c.res, (i * c.res_ld + j) * es);
+    q.pre = at(c.pre, (i * c.pre_ld + j) * es);
+    q.slope = at(c.slope, (i * c.slope_ld + j) * es);
+    q.out = at(c.out, (i * c.out_ld + j) * os);
+    return q;
+}
+// f(part) for all parts of at most `rows` x `cols`
+template <typename F>
+hipError_t by_parts(const LinearCall& c, int64_t rows, int64_t cols, F&& f) {
+    for (int64_t i = 0; i < c.rows; i += rows)
+        for (int64_t j = 0; j < c.cols; j += cols) {
+            const hipError_t e = f(part_of(c, i, c.rows - i < rows ? c.rows - i : rows, j, c.cols - j < cols ? c.cols - j : cols));
+            if (e != hipSuccess) return e;
+        }
+    return hipSuccess;
+}
 
 template <typename E, typename O>
 hipError_t join(const JoinParams& q, hipStream_t st) {
@@ -310,9 +344,7 @@ void pack(const void* src, int64_t ld, void* dst, int64_t rows, int64_t K, bool 
     hipLaunchKernelGGL((linear_pack_kernel<T>), dim3(grid), dim3(256), 0, st, (const T*)src, ld, (uint16_t*)dst, (int)r, (int)len, (int)packets, r * packets * 16);
 }
 
-}  // namespace
-
-hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
+hipError_t launch_piece(const LinearCall& c, void* ws, hipStream_t st) {
     const bool f32 = c.dtype == PURINE_F32;
     const int planes = f32 ? 3 : 1;
     const Finish f = finish_of(c);
@@ -381,6 +413,24 @@ hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
     JoinParams q{p.part, f, a, b, p.rows, p.cols, p.K, p.splits, 1};
     if (f32) return join<float, float>(q, st);
     return c.out_dtype == PURINE_F32 ? join<uint16_t, float>(q, st) : join<uint16_t, uint16_t>(q, st);
+}
+
+}  // namespace
+
+size_t linear_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_in, int dtype) {
+    if (rows <= MOST && cols <= MOST) return piece_ws_bytes(rows, cols, K, a_in, b_in, dtype);
+    size_t most = 0;
+    for (const int64_t r : {rows < MOST ? rows : MOST, rows % MOST})
+        for (const int64_t c : {cols < MOST ? cols : MOST, cols % MOST}) {
+            const size_t n = r && c ? piece_ws_bytes(r, c, K, a_in, b_in, dtype) : 0;
+            if (n > most) most = n;
+        }
+    return most;
+}
+
+hipError_t launch_linear(const LinearCall& c, void* ws, hipStream_t st) {
+    if (c.rows <= MOST && c.cols <= MOST) return launch_piece(c, ws, st);
+    return by_parts(c, MOST, MOST, [&](const LinearCall& q) { return launch_piece(q, ws, st); });
 }
 
 size_t act_bwd_ws_bytes(int64_t N, int64_t K) {
