@@ -419,20 +419,21 @@ __device__ __forceinline__ float2 group_averages(const NormParams& p, int lane, 
 // dscale and dshift of 16 channels: 16 threads each share the images and slices, and join in LDS.
 __device__ __forceinline__ void param_sums(const NormParams& p, int first) {
     __shared__ float2 sums[16][17];
-    const int l = threadIdx.x & 15, r = threadIdx.x >> 4, c = first + l;
+    const int l = threadIdx.x & 15, r = threadIdx.x >> 4;
+    const unsigned c = (unsigned)first + l;
     const int64_t rows = (int64_t)p.N * p.slices;
     float s = 0.0f, q = 0.0f;
-    if (c < p.C)
+    if (c < (unsigned)p.C)
 #pragma unroll 8
         for (int64_t k = r; k < rows; k += 16) { const float2 o = p.part[k * p.C + c]; s += o.x; q += o.y; }
     sums[r][l] = make_float2(s, q);
     __syncthreads();
-    if (r || c >= p.C) return;
+    if (r || c >= (unsigned)p.C) return;
     for (int k = 1; k < 16; ++k) { s += sums[k][l].x; q += sums[k][l].y; }
     p.dshift[c] = s;
     p.dscale[c] = q;
 }
-__global__ __launch_bounds__(NT) void norm_grad_params_kernel(const NormParams p) { param_sums(p, blockIdx.x * 16); }
+__global__ __launch_bounds__(NT) void norm_grad_params_kernel(const NormParams p, int from) { param_sums(p, from + (int)blockIdx.x * 16); }
 
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(NT) void norm_grad_apply_kernel(const NormParams p) {
@@ -697,6 +698,7 @@ HeldPlan held_plan(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, int v,
             const int64_t w = unit * m, cv = w / v;
             if (C % w) continue;
             if (w > 256 || cv > 256) break;
+            if (C / w > 1 << 21) continue;         // (workgroups of one image: below 2^31 threads)
             if (best.width && (w * bytes > 128 && best.width * bytes >= 64)) break;
             if (best.width && N * (C / w) < 512) break;
             const int threads = few || S * cv <= 256 * 4 ? 256 : HT;
@@ -776,7 +778,7 @@ int64_t held_blocks(NormParams& p, const HeldPlan& h) {
     return p.tiles;
 }
 // launch(parameters, workgroups) for all images, in as many calls as keep each below 2^31 threads (a launch ends at 2^32 of them: 2^24 images of a
-// workgroup each; an image has fewer).
+// workgroup each; one image has fewer in every form).
 template <typename T, typename F>
 hipError_t over_images(const NormParams& p, int64_t blocks, int threads, F&& launch) {
     const int64_t most = (((int64_t)1 << 31) / threads) / blocks, images = most < 1 ? 1 : most;
@@ -864,7 +866,11 @@ hipError_t launch_group_norm_bwd(int dtype, const NormShape& s, const void* x, c
         });
     });
     if (e != hipSuccess || !dscale) return e;
-    hipLaunchKernelGGL(norm_grad_params_kernel, dim3((p.C + 15) / 16), dim3(NT), 0, st, p);
+    constexpr int64_t MOST = 16 << 23;             // channels of a launch: below 2^32 threads
+    for (int64_t from = 0; from < p.C; from += MOST) {
+        const int64_t channels = p.C - from < MOST ? p.C - from : MOST;
+        hipLaunchKernelGGL(norm_grad_params_kernel, dim3((unsigned)((channels + 15) / 16)), dim3(NT), 0, st, p, (int)from);
+    }
     return hipGetLastError();
 }
 

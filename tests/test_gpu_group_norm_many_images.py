@@ -1,4 +1,4 @@
-"""Group normalization of more images than one launch can take a workgroup each of (2^32 threads), against 64 bits.
+"""Group normalization of more images, or channels, than one launch can take a workgroup of (2^32 threads), against 64 bits.
 
 Bounds as in test_gpu_group_norm.py: results in bf16 are rounded once, 2^-8.5 in the 2-norm; fp32 statistics are within 32 eps."""
 import pytest
@@ -31,3 +31,23 @@ def test_more_than_two_to_the_24():
         assert float((y[part].double() - wy[:, 0]).norm()) <= 2 ** -8.5 * float(wy.norm())
         wdx, *_, hnorm = ref.group_norm_grad(d[0], s, b, G, 1e-2, "silu", d[1])
         assert float((dx[part].double() - wdx[:, 0]).norm()) <= 2 ** -8.5 * float(hnorm)
+
+
+def test_parameters_of_two_to_the_28_channels():
+    import paper_1412_6249_amd as pa
+    C = (1 << 28) + 48
+    G = C // 16
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x, dy = (torch.randn(1, C, generator=g, device=DEV) for _ in range(2))
+    ws = torch.empty(max(pa.purine_group_norm_workspace_bytes(b, (1, C), G) for b in (0, 1)), dtype=torch.uint8, device=DEV)
+    y = torch.empty_like(x)
+    mean, rstd = (torch.empty(1, G, device=DEV) for _ in range(2))
+    ds, db = (torch.full((C,), float("nan"), device=DEV) for _ in range(2))
+    pa.purine_group_norm_fwd(x, None, None, y, mean, rstd, G, 1e-2, pa.PURINE_ACT_NONE, ws=ws)
+    pa.purine_group_norm_bwd(x, None, None, mean, rstd, dy, torch.empty_like(x), ds, db, G, pa.PURINE_ACT_NONE, ws=ws)
+    assert torch.equal(db, dy[0])                        # one image of one position
+    for k in range(0, C, 1 << 24):
+        part = slice(k, min(C, k + (1 << 24)))
+        xhat = (x[0, part].double().reshape(-1, 16) - mean[0, k // 16:part.stop // 16, None]) * rstd[0, k // 16:part.stop // 16, None]
+        want = dy[0, part].double() * xhat.reshape(-1)
+        assert bool(((ds[part].double() - want).abs() <= 8 * EPS * dy[0, part].double().abs() * (xhat.reshape(-1).abs() + 1)).all())
