@@ -16,6 +16,7 @@ namespace purine {
 namespace {
 
 constexpr int NT = 256, PER = 8, CHUNK = NT * PER, TABLE = 40;
+constexpr unsigned MOST = 1u << 22;        // workgroups of a launch, the last tensor's (2^20 at most) aside: a launch ends at 2^32 threads
 static_assert(PURINE_ADAMW_BLOCK == 32 * PER, "a block's elements lie in half a wavefront");
 
 struct AdamwTensor {
@@ -260,21 +261,21 @@ hipError_t launch_adamw(const purine_adamw_desc& d, const purine_adamw_param* pa
     p.dither = d.dither;
     (void)hipGetLastError();
     ProbeScope probe(st);
-    for (int from = 0; from < n; from += TABLE) {
-        p.count = n - from < TABLE ? n - from : TABLE;
+    for (int from = 0; from < n; from += p.count) {
+        p.count = 0;
         p.ordinal = (unsigned)from;
         unsigned grid = 0;
         bool coded = false;
-        for (int i = 0; i < p.count; ++i) {
-            const purine_adamw_param& q = params[from + i];
-            AdamwTensor& o = p.t[i];
+        for (; p.count < TABLE && from + p.count < n && grid < MOST; ++p.count) {
+            const purine_adamw_param& q = params[from + p.count];
+            AdamwTensor& o = p.t[p.count];
             o.w = q.w.data; o.dw = q.dw.data; o.m = q.m.data; o.v = q.v.data;
             o.copy = (uint16_t*)q.copy.data;
             coded = q.m.dtype == PURINE_F8;
             o.ms = coded ? (float*)q.m_scale.data : nullptr;
             o.vs = coded ? (float*)q.v_scale.data : nullptr;
             o.n = (unsigned)elements(q.w);
-            p.first[i] = grid;
+            p.first[p.count] = grid;
             grid += (o.n + CHUNK - 1) / CHUNK;
         }
         const bool w16 = params[from].w.dtype == PURINE_BF16, d16 = params[from].dw.dtype == PURINE_BF16;
