@@ -158,7 +158,12 @@ DirectForm direct_form(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_
         return 3.8 + (double)each * fmax(alone, full * load) + 0.4 * load;
     };
     if (a_in && b_in) {
-        if (rows <= 4 && K % (f32 ? 4 : 8) == 0) offer(DIRECT_ROW, 4.0 + (double)cols * (double)K * (f32 ? 4.0 : 2.0) / (rows > 2 && !f32 ? 3.6e6 : 5.0e6));
+        if (rows <= 4 && K % (f32 ? 4 : 8) == 0) {
+            // reading B, or what a column costs however short it is (2^20 columns of 64: bf16 284, 549 and 1451 us with 1, 2 and 4 rows, fp32 157, 323 and 1354)
+            const double read = (double)K * (f32 ? 4.0 : 2.0) / (rows > 2 && !f32 ? 3.6e6 : 5.0e6);
+            const double column = rows > 2 ? 1.35e-3 : (f32 ? 0.15e-3 : 0.27e-3) * (double)rows;
+            offer(DIRECT_ROW, 4.0 + (double)cols * fmax(read, column));
+        }
         if (rows <= 16) offer(DIRECT_ROWS, chain((cols + 15) / 16, 8, 4, f32 ? 0.75 : 0.29, f32 ? 1.08 : 0.47));
     }
     const int64_t groups = ((rows + 31) / 32) * ((cols + 31) / 32);
