@@ -360,6 +360,11 @@ hipError_t launch_piece(const LinearCall& c, void* ws, hipStream_t st) {
     const int64_t span = ((c.a_in ? c.rows : c.K) * c.a_ld > (c.b_in ? c.cols : c.K) * c.b_ld ? (c.a_in ? c.rows : c.K) * c.a_ld : (c.b_in ? c.cols : c.K) * c.b_ld) * es;
     if (direct == DIRECT_STREAM) return launch_linear_stream(c, st);
     if (direct != DIRECT_NONE && span < 0x7fffffff) return launch_linear_direct(c, direct, st);
+    if (direct != DIRECT_NONE && c.a_in && c.b_in && c.a_ld < far && c.b_ld < far) {
+        // as many rows of either operand as 32-bit offsets reach, in eights, whose results begin at 16 bytes (24 at least)
+        const int64_t rows = 0x7ffffff0 / (c.a_ld * es) / 8 * 8, cols = 0x7ffffff0 / (c.b_ld * es) / 8 * 8;
+        return by_parts(c, rows, cols, [&](const LinearCall& q) { return launch_linear_direct(q, direct, st); });
+    }
     if (direct != DIRECT_NONE || c.a_ld >= far || c.b_ld >= far) {
         FarParams p{a, b, f, (int)c.rows, (int)c.cols, (int)c.K, (int)((c.cols + TS - 1) / TS)};
         const unsigned grid = (unsigned)((c.rows + TS - 1) / TS * p.tiles_j);
