@@ -151,25 +151,26 @@ __device__ __forceinline__ void join_moments(float2* sums, int width, int R, int
 template <typename Sum, typename Mean, typename Squares>
 __device__ __forceinline__ float2 group_stats(const NormParams& p, int lane, int lanes, Sum&& sum, Mean&& mean, Squares&& squares) {
     float all = 0.0f, var = 0.0f;
-    for (int c = lane; c < p.per; c += lanes) all += mean(c);
+    for (unsigned c = lane; c < (unsigned)p.per; c += lanes) all += mean(c);
     const float mu = sum(all) / (float)p.per;
-    for (int c = lane; c < p.per; c += lanes) var += squares(c, mu) / (float)p.S;
+    for (unsigned c = lane; c < (unsigned)p.per; c += lanes) var += squares(c, mu) / (float)p.S;
     var = sum(var) / (float)p.per;
     return make_float2(mu, 1.0f / sqrtf(var + p.eps));
 }
 
 // What a workgroup of the kernels over slices works on (image, slice of the positions, tile of the channels), the channels of this thread, its
-// place among the threads that share them, and their number.
+// place among the threads that share them, and their number. Positions count from the slice's first, so that the sums of them below stay far from 2^31.
 template <int V>
 struct Place {
-    int n, slice, s0, s1, c, r, R, tile, c0, c1;        // c0 .. c1 - 1: the tile's channels
+    int n, slice, len, c, r, R, tile, c0, c1;           // len: positions; c0 .. c1 - 1: the tile's channels
+    int64_t at;                                         // elements from the image's first to the slice's first of these channels
     bool on;
     __device__ __forceinline__ explicit Place(const NormParams& p) {
         const int b = blockIdx.x / p.tiles, cv = p.C / V, first = (int)(blockIdx.x - b * p.tiles) * NT;
         n = b / p.slices;
         slice = b - n * p.slices;
-        s0 = slice * p.rows;
-        s1 = min(s0 + p.rows, p.S);
+        const int s0 = slice * p.rows;
+        len = min(p.rows, p.S - s0);
         tile = min(NT, cv - first);
         R = NT / tile;
         r = threadIdx.x / tile;
@@ -177,6 +178,7 @@ struct Place {
         c = (first + (int)threadIdx.x % tile) * V;
         c0 = first * V;
         c1 = c0 + tile * V;
+        at = (int64_t)s0 * p.C + c;
     }
 };
 
@@ -204,20 +206,20 @@ template <typename T, int V>
 __global__ __launch_bounds__(NT) void norm_sums_kernel(const NormParams p) {
     __shared__ float2 sums[NT * V];
     const Place<V> at(p);
-    const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
+    const T* x = (const T*)p.x + at.n * p.x_ns + at.at;
     float k[V], mean[V], m2[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) mean[i] = m2[i] = k[i] = 0.0f;
     if (at.on) {
-        load_v<T, V>(x, k);
+        load_v<T, V>((const T*)p.x + at.n * p.x_ns + at.c, k);
         Pack<T, V> in[AHEAD], next[AHEAD];
         auto load = [&](int t) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) next[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(t + u * at.R, at.s1 - 1) * p.C);
+            for (int u = 0; u < AHEAD; ++u) next[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(t + u * at.R, at.len - 1) * p.C);
         };
         float before = 0.0f;
-        load(at.s0 + at.r);
-        for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
+        load(at.r);
+        for (int t = at.r; t < at.len; t += AHEAD * at.R) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) in[u] = next[u];
             load(t + AHEAD * at.R);
@@ -227,7 +229,7 @@ __global__ __launch_bounds__(NT) void norm_sums_kernel(const NormParams p) {
             for (int i = 0; i < V; ++i) s[i] = q[i] = 0.0f;
 #pragma unroll
             for (int u = 1; u < AHEAD; ++u) {
-                if (t + u * at.R >= at.s1) break;
+                if (t + u * at.R >= at.len) break;
                 float v[V];
                 widen_v<T, V>(in[u], v);
 #pragma unroll
@@ -246,7 +248,7 @@ __global__ __launch_bounds__(NT) void norm_sums_kernel(const NormParams p) {
 #pragma unroll
         for (int i = 0; i < V; ++i) sums[threadIdx.x * V + i] = make_float2(mean[i], m2[i]);
     }
-    join_moments<NT>(sums, at.tile * V, at.R, at.s1 - at.s0);
+    join_moments<NT>(sums, at.tile * V, at.R, at.len);
     if (at.r != 0) return;
     float2* o = p.part + ((int64_t)at.n * p.slices + at.slice) * p.C + at.c;
 #pragma unroll
@@ -324,15 +326,15 @@ __global__ __launch_bounds__(NT) void norm_apply_kernel(const NormParams p) {
         const float2 o = stat[(at.c + i) / p.per - g0];
         mu[i] = o.x; a[i] = o.y * scale_of(p, at.c + i); b[i] = shift_of(p, at.c + i);
     }
-    const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
-    T* y = (T*)p.out + at.n * p.out_ns + at.c;
-    for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
+    const T* x = (const T*)p.x + at.n * p.x_ns + at.at;
+    T* y = (T*)p.out + at.n * p.out_ns + at.at;
+    for (int t = at.r; t < at.len; t += AHEAD * at.R) {
         Pack<T, V> in[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) in[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(t + u * at.R, at.s1 - 1) * p.C);
+        for (int u = 0; u < AHEAD; ++u) in[u] = *reinterpret_cast<const Pack<T, V>*>(x + (int64_t)min(t + u * at.R, at.len - 1) * p.C);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            if (t + u * at.R >= at.s1) break;
+            if (t + u * at.R >= at.len) break;
             float v[V];
             widen_v<T, V>(in[u], v);
 #pragma unroll
@@ -363,26 +365,26 @@ __global__ __launch_bounds__(NT, 4) void norm_grad_sums_kernel(const NormParams 
             const int g = at.n * p.G + (at.c + i) / p.per;
             mu[i] = p.mean[g]; rstd[i] = p.rstd[g]; sc[i] = scale_of(p, at.c + i); sh[i] = shift_of(p, at.c + i);
         }
-        const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
-        const T* dy = (const T*)p.dy + at.n * p.dy_ns + at.c;
+        const T* x = (const T*)p.x + at.n * p.x_ns + at.at;
+        const T* dy = (const T*)p.dy + at.n * p.dy_ns + at.at;
         // (a batch of positions ahead of its use: 64 x 12544 x 64 in bf16 43.8 us, without 53.6; its 206 MB at the rate of a copy 40)
         Pack<T, V> in[BATCH], gr[BATCH], in_next[BATCH], gr_next[BATCH];
         auto load = [&](int t) {
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
-                const int64_t row = (int64_t)min(t + u * at.R, at.s1 - 1) * p.C;
+                const int64_t row = (int64_t)min(t + u * at.R, at.len - 1) * p.C;
                 in_next[u] = *reinterpret_cast<const Pack<T, V>*>(x + row);
                 gr_next[u] = *reinterpret_cast<const Pack<T, V>*>(dy + row);
             }
         };
-        load(at.s0 + at.r);
-        for (int t = at.s0 + at.r; t < at.s1; t += BATCH * at.R) {
+        load(at.r);
+        for (int t = at.r; t < at.len; t += BATCH * at.R) {
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) { in[u] = in_next[u]; gr[u] = gr_next[u]; }
             load(t + BATCH * at.R);
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
-                if (t + u * at.R >= at.s1) break;
+                if (t + u * at.R >= at.len) break;
                 float v[V], d[V];
                 widen_v<T, V>(in[u], v);
                 widen_v<T, V>(gr[u], d);
@@ -406,7 +408,7 @@ __global__ __launch_bounds__(NT, 4) void norm_grad_sums_kernel(const NormParams 
 template <typename Sum, typename Channel>
 __device__ __forceinline__ float2 group_averages(const NormParams& p, int lane, int lanes, Sum&& sum, Channel&& channel) {
     float a = 0.0f, b = 0.0f;
-    for (int c = lane; c < p.per; c += lanes) {
+    for (unsigned c = lane; c < (unsigned)p.per; c += lanes) {
         float w;
         const float2 o = channel(c, w);
         a += o.x * w;
@@ -455,20 +457,20 @@ __global__ __launch_bounds__(NT) void norm_grad_apply_kernel(const NormParams p)
         mu[i] = p.mean[g]; rstd[i] = p.rstd[g]; sc[i] = scale_of(p, at.c + i); sh[i] = shift_of(p, at.c + i);
         c1[i] = rstd[i] * o.x; c2[i] = rstd[i] * o.y; rs[i] = rstd[i] * sc[i];
     }
-    const T* x = (const T*)p.x + at.n * p.x_ns + at.c;
-    const T* dy = (const T*)p.dy + at.n * p.dy_ns + at.c;
-    T* dx = (T*)p.out + at.n * p.out_ns + at.c;
-    for (int t = at.s0 + at.r; t < at.s1; t += AHEAD * at.R) {
+    const T* x = (const T*)p.x + at.n * p.x_ns + at.at;
+    const T* dy = (const T*)p.dy + at.n * p.dy_ns + at.at;
+    T* dx = (T*)p.out + at.n * p.out_ns + at.at;
+    for (int t = at.r; t < at.len; t += AHEAD * at.R) {
         Pack<T, V> in[AHEAD], gr[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const int64_t row = (int64_t)min(t + u * at.R, at.s1 - 1) * p.C;
+            const int64_t row = (int64_t)min(t + u * at.R, at.len - 1) * p.C;
             in[u] = *reinterpret_cast<const Pack<T, V>*>(x + row);
             gr[u] = *reinterpret_cast<const Pack<T, V>*>(dy + row);
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            if (t + u * at.R >= at.s1) break;
+            if (t + u * at.R >= at.len) break;
             T* o = dx + (int64_t)(t + u * at.R) * p.C;
             float v[V], d[V], old[V];
             widen_v<T, V>(in[u], v);
@@ -759,8 +761,8 @@ NormParams params_of(const NormShape& s, void* ws) {
     p.eps = s.eps;
     p.x_ns = s.x_ns; p.dy_ns = s.dy_ns;
     p.slices = slices_of(s.N, s.S, s.C);
-    p.rows = (s.S + p.slices - 1) / p.slices;
-    p.slices = (s.S + p.rows - 1) / p.rows;
+    p.rows = (s.S - 1) / p.slices + 1;
+    p.slices = (s.S - 1) / p.rows + 1;
     p.part = (float2*)ws;
     p.about = (float*)(p.part + (int64_t)s.N * p.slices * s.C);
     return p;
@@ -768,7 +770,7 @@ NormParams params_of(const NormShape& s, void* ws) {
 
 // Workgroups of an image in the kernels that walk over positions, and in the held ones.
 int64_t blocks_of(NormParams& p, int v) {
-    p.tiles = (p.C / v + NT - 1) / NT;
+    p.tiles = (p.C / v - 1) / NT + 1;
     return (int64_t)p.slices * p.tiles;
 }
 int64_t held_blocks(NormParams& p, const HeldPlan& h) {

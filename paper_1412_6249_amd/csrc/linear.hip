@@ -19,11 +19,13 @@ __global__ __launch_bounds__(256) void linear_far_kernel(const FarParams p) {
     const T* a = (const T*)p.a.p;
     const T* b = (const T*)p.b.p;
     float acc[4][4] = {};
-    for (int k0 = 0; k0 < p.K; k0 += KS) {
+    const unsigned K = p.K;            // (k0 + k passes 2^31 where K is near it)
+    for (unsigned k0 = 0; k0 < K; k0 += KS) {
         for (int e = threadIdx.x; e < KS * TS; e += 256) {
-            const int k = e / TS, i = e % TS;
-            as[k][i] = k0 + k < p.K && i0 + i < p.rows ? widen<T>(a[(i0 + i) * p.a.i_step + (k0 + k) * p.a.k_step]) : 0.0f;
-            bs[k][i] = k0 + k < p.K && j0 + i < p.cols ? widen<T>(b[(j0 + i) * p.b.i_step + (k0 + k) * p.b.k_step]) : 0.0f;
+            const unsigned k = e / TS;
+            const int i = e % TS;
+            as[k][i] = k0 + k < K && i0 + i < p.rows ? widen<T>(a[(i0 + i) * p.a.i_step + (k0 + k) * p.a.k_step]) : 0.0f;
+            bs[k][i] = k0 + k < K && j0 + i < p.cols ? widen<T>(b[(j0 + i) * p.b.i_step + (k0 + k) * p.b.k_step]) : 0.0f;
         }
         __syncthreads();
         for (int k = 0; k < KS; ++k)
@@ -201,27 +203,27 @@ __global__ __launch_bounds__(ANT) void act_bwd_kernel(const ActParams p) {
     __shared__ float sums[ANT * V];
     const int slice = blockIdx.x / p.tiles, first = (int)(blockIdx.x - (unsigned)slice * p.tiles) * ANT;
     const int tile = min(ANT, p.K / V - first), R = ANT / tile, r = threadIdx.x / tile, j = (first + (int)threadIdx.x % tile) * V;
-    const int i1 = min((slice + 1) * p.rows, p.N);
+    const int i0 = slice * p.rows, n = min(p.rows, p.N - i0);         // rows from i0 on (counted from there: sums stay far from 2^31)
     float sum[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) sum[e] = 0.0f;
     if (r < R) {
-        const T* dy = (const T*)p.dy + j;
-        const T* pre = (const T*)p.pre + j;
-        T* g = (T*)p.g + j;
+        const T* dy = (const T*)p.dy + i0 * p.dy_ld + j;
+        const T* pre = (const T*)p.pre + i0 * p.pre_ld + j;
+        T* g = (T*)p.g + i0 * p.g_ld + j;
         constexpr int AHEAD = 4;
-        for (int i = slice * p.rows + r; i < i1; i += R * AHEAD) {
+        for (int i = r; i < n; i += R * AHEAD) {
             float v[AHEAD][V], z[AHEAD][V];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                const int64_t row = min(i + u * R, i1 - 1);
+                const int64_t row = min(i + u * R, n - 1);
                 lin::get_v(dy + row * p.dy_ld, v[u]);
                 if (ACT != PURINE_ACT_NONE) lin::get_v(pre + row * p.pre_ld, z[u]);
             }
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const int64_t row = i + u * R;
-                if (row >= i1) break;
+                if (row >= n) break;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     if (ACT != PURINE_ACT_NONE) v[u][e] *= act_slope<ACT>(z[u][e]);
@@ -456,7 +458,7 @@ namespace {
 template <typename T, int V>
 void act_bwd(const ActParams& q, int act, hipStream_t st) {
     ActParams p = q;
-    p.tiles = (p.K / V + ANT - 1) / ANT;
+    p.tiles = (p.K / V - 1) / ANT + 1;
     const unsigned grid = (unsigned)((int64_t)p.slices * p.tiles);
     switch (act) {
         case PURINE_ACT_RELU: hipLaunchKernelGGL((act_bwd_kernel<T, V, PURINE_ACT_RELU>), dim3(grid), dim3(ANT), 0, st, p); break;
