@@ -11,7 +11,7 @@ struct NormShape {
     float eps;
     int act;
 };
-size_t group_norm_ws_bytes(int64_t N, int64_t S, int64_t C);
+size_t group_norm_ws_bytes(int64_t N, int64_t S, int64_t C, int64_t G);
 hipError_t launch_group_norm_fwd(int dtype, const NormShape& s, const void* x, const float* scale, const float* shift, void* y, float* mean,
                                  float* rstd, void* ws, hipStream_t st);
 hipError_t launch_group_norm_bwd(int dtype, const NormShape& s, const void* x, const float* scale, const float* shift, const float* mean,

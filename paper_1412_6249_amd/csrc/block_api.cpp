@@ -123,7 +123,7 @@ size_t purine_group_norm_workspace_bytes(int backward, const int64_t x_dim[4], i
     }
     const int64_t C = x_dim[ndim - 1];
     if (C % groups) return 0;
-    return group_norm_ws_bytes(x_dim[0], n / x_dim[0] / C, C);
+    return group_norm_ws_bytes(x_dim[0], n / x_dim[0] / C, C, groups);
 }
 
 int purine_group_norm_fwd(const purine_tensor* x, const purine_tensor* scale, const purine_tensor* shift, purine_tensor* y,
@@ -139,7 +139,7 @@ int purine_group_norm_fwd(const purine_tensor* x, const purine_tensor* scale, co
     if (mean && ((rc = norm_stat(mean, s)) || (rc = norm_stat(rstd, s)))) return rc;
     if (norm_aliased_badly(y, x) || any_meets(y, {scale, shift, mean, rstd})) return PURINE_E_LAYOUT;
     if (mean && (any_meets(mean, {x, scale, shift, rstd}) || any_meets(rstd, {x, scale, shift}))) return PURINE_E_LAYOUT;
-    const size_t need = group_norm_ws_bytes(s.N, s.S, s.C);
+    const size_t need = group_norm_ws_bytes(s.N, s.S, s.C, s.G);
     if ((rc = check_ws(ws, ws_bytes, need, {x, y, scale, shift, mean, rstd}))) return rc;
     s.y_ns = nstride_of(y);
     s.eps = eps;
@@ -163,7 +163,7 @@ int purine_group_norm_bwd(const purine_tensor* x, const purine_tensor* scale, co
     if (norm_aliased_badly(dx, dy) || overlaps(dx, x) || any_meets(dx, {scale, shift, mean, rstd, dscale, dshift})) return PURINE_E_LAYOUT;
     if (dscale && (any_meets(dscale, {x, scale, shift, mean, rstd, dy, dshift}) || any_meets(dshift, {x, scale, shift, mean, rstd, dy})))
         return PURINE_E_LAYOUT;
-    const size_t need = group_norm_ws_bytes(s.N, s.S, s.C);
+    const size_t need = group_norm_ws_bytes(s.N, s.S, s.C, s.G);
     if ((rc = check_ws(ws, ws_bytes, need, {x, scale, shift, mean, rstd, dy, dx, dscale, dshift}))) return rc;
     s.dy_ns = nstride_of(dy);
     s.dx_ns = nstride_of(dx);

@@ -16,7 +16,7 @@
 //
 // Where an image's share of a few whole groups fits a workgroup's registers (norm_held_kernel, norm_grad_held_kernel), one workgroup reads it once and
 // writes the results: every tensor moves once. Otherwise (norm_sums / norm_apply) one kernel sums over slices of the positions and a second
-// one joins the slices for itself and reads its tensors again, if they are not too large from the last-level cache.
+// one joins the slices for itself, or finds them joined by norm_join, and reads its tensors again, if they are not too large from the last-level cache.
 #include "activation.h"
 #include "bf16.h"
 #include "block.h"
@@ -79,11 +79,14 @@ struct NormParams {
     const float* scale; const float* shift;     // or null
     float2* part;              // per image, slice and channel: mean and sum of squares about it, or the gradient's two sums
     float* about;              // per image and channel: the value that the means are relative to
+    float2* stat;              // per image and group: mean and rstd, or the gradient's averages, where a kernel of their own joins them; else null
+    float4* chunk;             // of that kernel: what its workgroups make of their part of a group
     const float* mean; const float* rstd;       // gradient: as saved
     float* mean_out; float* rstd_out;           // or null
     float* dscale; float* dshift;               // or null
     int N, S, C, G, per;       // channels per group
     int slices, rows;          // slices of the positions, positions per slice
+    int chunks;                // workgroups that join a group's sums
     int tiles;                 // of NT vectors of channels
     int width;                 // held kernels: channels of a workgroup
     float eps;
@@ -296,7 +299,8 @@ __global__ __launch_bounds__(NT) void norm_apply_kernel(const NormParams p) {
     __shared__ float2 stat[NT * V + 1];
     const Place<V> at(p);
     const int g0 = at.c0 / p.per, g1 = (at.c1 - 1) / p.per;
-    for_groups<NT>(g1 - g0 + 1, p.per, [&](int g, int lane, int lanes, auto&& sum) {
+    if (p.stat) for (int g = threadIdx.x; g <= g1 - g0; g += NT) stat[g] = p.stat[at.n * p.G + g0 + g];
+    else for_groups<NT>(g1 - g0 + 1, p.per, [&](int g, int lane, int lanes, auto&& sum) {
         const int first = (g0 + g) * p.per;
         const float* about = p.about + (int64_t)at.n * p.C + first;
         const float2* part = p.part + (int64_t)at.n * p.slices * p.C + first;
@@ -442,7 +446,8 @@ __global__ __launch_bounds__(NT) void norm_grad_apply_kernel(const NormParams p)
     __shared__ float2 stat[NT * V + 1];
     const Place<V> at(p);
     const int g0 = at.c0 / p.per, g1 = (at.c1 - 1) / p.per;
-    for_groups<NT>(g1 - g0 + 1, p.per, [&](int g, int lane, int lanes, auto&& sum) {
+    if (p.stat) for (int g = threadIdx.x; g <= g1 - g0; g += NT) stat[g] = p.stat[at.n * p.G + g0 + g];
+    else for_groups<NT>(g1 - g0 + 1, p.per, [&](int g, int lane, int lanes, auto&& sum) {
         const int first = (g0 + g) * p.per;
         const float2 o = group_averages(p, lane, lanes, sum, [&](int c, float& w) { w = scale_of(p, first + c); return over_slices(p, at.n, first + c); });
         if (lane == 0) stat[g] = o;
@@ -485,6 +490,99 @@ __global__ __launch_bounds__(NT) void norm_grad_apply_kernel(const NormParams p)
             }
             store_v<T, V>(o, v);
         }
+    }
+}
+
+// ---- the sums of long groups, joined once
+constexpr int CHUNK = NT * 64;                 // pairs of sums of a workgroup at most
+
+// The sum over the workgroup's threads, in a fixed order, in every thread.
+__device__ __forceinline__ float sum_over_block(float v, float* sums) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = sums[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) v += sums[w];
+    return v;
+}
+// Number, mean and sum of squares about it of `count` members: member(i, n, mean about the first member's, squares).
+template <typename Member>
+__device__ __forceinline__ float3 join_members(unsigned count, float* sums, Member&& member) {
+    float n, m, q, all = 0.0f, s = 0.0f;
+    for (unsigned i = threadIdx.x; i < count; i += NT) { member(i, n, m, q); all += n; s += n * m; }
+    all = sum_over_block(all, sums);
+    const float mean = sum_over_block(s, sums) / all;
+    s = 0.0f;
+    for (unsigned i = threadIdx.x; i < count; i += NT) { member(i, n, m, q); s += q + n * ((m - mean) * (m - mean)); }
+    return make_float3(all, mean, sum_over_block(s, sums));
+}
+__device__ __forceinline__ void put_stats(const NormParams& p, unsigned group, float mean, float var) {
+    if (threadIdx.x) return;
+    const float2 o = make_float2(mean, 1.0f / sqrtf(var + p.eps));
+    p.stat[group] = o;
+    if (p.mean_out) { p.mean_out[group] = o.x; p.rstd_out[group] = o.y; }
+}
+// A workgroup per CHUNK of a group's slices x channels, whose results are those of the group if there is one.
+template <bool GRAD>
+__global__ __launch_bounds__(NT) void norm_join_kernel(const NormParams p) {
+    __shared__ float sums[NT / 64];
+    const unsigned group = blockIdx.x / p.chunks, first = (blockIdx.x - group * p.chunks) * CHUNK, per = p.per;
+    const unsigned n = group / p.G, c0 = (group - n * p.G) * per, count = min((unsigned)CHUNK, p.slices * per - first);
+    const float2* part = p.part + (int64_t)n * p.slices * p.C + c0;
+    auto place = [=](unsigned i, unsigned& slice, unsigned& c) { slice = (first + i) / per; c = first + i - slice * per; };
+    if constexpr (GRAD) {
+        float a = 0.0f, b = 0.0f;
+#pragma unroll 4
+        for (unsigned i = threadIdx.x; i < count; i += NT) {
+            unsigned s, c;
+            place(i, s, c);
+            const float2 o = part[(int64_t)s * p.C + c];
+            const float w = scale_of(p, (int)(c0 + c));
+            a += o.x * w;
+            b += o.y * w;
+        }
+        a = sum_over_block(a, sums);
+        b = sum_over_block(b, sums);
+        const float all = (float)per * (float)p.S;
+        if (threadIdx.x) return;
+        if (p.chunks == 1) p.stat[group] = make_float2(a / all, b / all);
+        else p.chunk[blockIdx.x] = make_float4(a, b, 0.0f, 0.0f);
+    } else {
+        const float* about = p.about + (int64_t)n * p.C + c0;
+        unsigned s, c;
+        place(0, s, c);
+        const float zero = about[c] + part[(int64_t)s * p.C + c].x, rows = (float)p.rows, rest = (float)(p.S - (p.slices - 1) * p.rows);
+        const float3 o = join_members(count, sums, [&](unsigned i, float& k, float& m, float& q) {
+            unsigned s, c;
+            place(i, s, c);
+            const float2 v = part[(int64_t)s * p.C + c];
+            k = (int)s == p.slices - 1 ? rest : rows;
+            m = (about[c] - zero) + v.x;
+            q = v.y;
+        });
+        if (p.chunks == 1) put_stats(p, group, zero + o.y, o.z / o.x);
+        else if (threadIdx.x == 0) p.chunk[blockIdx.x] = make_float4(o.x, zero + o.y, o.z, 0.0f);
+    }
+}
+// The same of a group's chunks.
+template <bool GRAD>
+__global__ __launch_bounds__(NT) void norm_join_chunks_kernel(const NormParams p) {
+    __shared__ float sums[NT / 64];
+    const float4* chunk = p.chunk + (int64_t)blockIdx.x * p.chunks;
+    if constexpr (GRAD) {
+        float a = 0.0f, b = 0.0f;
+        for (int i = threadIdx.x; i < p.chunks; i += NT) { a += chunk[i].x; b += chunk[i].y; }
+        a = sum_over_block(a, sums);
+        b = sum_over_block(b, sums);
+        const float all = (float)p.per * (float)p.S;
+        if (threadIdx.x == 0) p.stat[blockIdx.x] = make_float2(a / all, b / all);
+    } else {
+        const float zero = chunk[0].y;
+        const float3 o = join_members(p.chunks, sums, [&](unsigned i, float& n, float& m, float& q) { const float4 v = chunk[i]; n = v.x; m = v.y - zero; q = v.z; });
+        put_stats(p, blockIdx.x, zero + o.y, o.z / o.x);
     }
 }
 
@@ -755,17 +853,51 @@ hipError_t by_pieces(const HeldPlan& h, F&& f) {
     return hipErrorInvalidValue;
 }
 
+// Slices, and where the scratch has what. The kernels that use a group's sums join them for themselves, which saves a launch, unless a thread would go
+// through more than LONG slices for it. us, bf16, both directions, for themselves / by kernels of their own: 64 in turn 16 x 12544 x 64 in one group 68 / 75; 128
+// 16 x 4096 x 320 in 32 groups 123 / 93, 8 x 12544 x 64 62 / 53; 2048 2 x 65536 x 2048 in 32 groups 2220 / 920.
+constexpr int64_t LONG = 64;
+struct SlicedPlan { int rows, slices, chunks; size_t about, stat, chunk, bytes; };
+SlicedPlan sliced_plan(int64_t N, int64_t S, int64_t C, int64_t G) {
+    SlicedPlan o{};
+    o.rows = (int)((S - 1) / slices_of(N, S, C) + 1);
+    o.slices = (int)((S - 1) / o.rows + 1);
+    const int64_t per = C / G, pairs = o.slices * per;
+    int64_t lanes = 1;
+    while (lanes < 64 && lanes < per) lanes *= 2;
+    const int64_t groups = per < 1024 ? (C < 1024 ? C : 1024) / per : 1;       // of a tile of channels
+    if (o.slices * ((per + lanes - 1) / lanes) * ((groups * lanes + NT - 1) / NT) > LONG) o.chunks = (int)((pairs + CHUNK - 1) / CHUNK);
+    auto whole = [](size_t n) { return (n + 15) / 16 * 16; };
+    o.about = whole((size_t)(N * o.slices * C) * sizeof(float2));
+    o.stat = o.about + whole((size_t)(N * C) * sizeof(float));
+    o.chunk = o.stat + (o.chunks ? whole((size_t)(N * G) * sizeof(float2)) : 0);
+    o.bytes = o.chunk + (o.chunks > 1 ? (size_t)(N * G * o.chunks) * sizeof(float4) : 0);
+    return o;
+}
+
 NormParams params_of(const NormShape& s, void* ws) {
     NormParams p{};
     p.N = s.N; p.S = s.S; p.C = s.C; p.G = s.G; p.per = s.C / s.G;
     p.eps = s.eps;
     p.x_ns = s.x_ns; p.dy_ns = s.dy_ns;
-    p.slices = slices_of(s.N, s.S, s.C);
-    p.rows = (s.S - 1) / p.slices + 1;
-    p.slices = (s.S - 1) / p.rows + 1;
-    p.part = (float2*)ws;
-    p.about = (float*)(p.part + (int64_t)s.N * p.slices * s.C);
+    const SlicedPlan plan = sliced_plan(s.N, s.S, s.C, s.G);
+    p.rows = plan.rows;
+    p.slices = plan.slices;
+    p.chunks = plan.chunks;
+    char* const scratch = (char*)ws;
+    p.part = (float2*)scratch;
+    p.about = (float*)(scratch + plan.about);
+    p.stat = plan.chunks ? (float2*)(scratch + plan.stat) : nullptr;
+    p.chunk = (float4*)(scratch + plan.chunk);
     return p;
+}
+// Joins the groups' sums of the images of a call.
+template <bool GRAD>
+void join_groups(const NormParams& p, hipStream_t st) {
+    if (!p.stat) return;
+    const unsigned groups = (unsigned)p.N * (unsigned)p.G;
+    hipLaunchKernelGGL((norm_join_kernel<GRAD>), dim3(groups * (unsigned)p.chunks), dim3(NT), 0, st, p);
+    if (p.chunks > 1) hipLaunchKernelGGL((norm_join_chunks_kernel<GRAD>), dim3(groups), dim3(NT), 0, st, p);
 }
 
 // Workgroups of an image in the kernels that walk over positions, and in the held ones.
@@ -795,6 +927,7 @@ hipError_t over_images(const NormParams& p, int64_t blocks, int threads, F&& lau
         if (p.mean_out) { q.mean_out += groups; q.rstd_out += groups; }
         q.part += n * p.slices * p.C;
         q.about += n * p.C;
+        if (p.stat) q.stat += groups;
         const hipError_t e = launch(q, dim3((unsigned)(q.N * blocks)));
         if (e != hipSuccess) return e;
     }
@@ -804,7 +937,7 @@ hipError_t over_images(const NormParams& p, int64_t blocks, int threads, F&& lau
 }  // namespace
 
 // What the sliced kernels take, whichever a call gets (the held ones need a slice's at most).
-size_t group_norm_ws_bytes(int64_t N, int64_t S, int64_t C) { return (size_t)(N * slices_of(N, S, C) * C) * sizeof(float2) + (size_t)(N * C) * sizeof(float); }
+size_t group_norm_ws_bytes(int64_t N, int64_t S, int64_t C, int64_t G) { return sliced_plan(N, S, C, G).bytes; }
 
 hipError_t launch_group_norm_fwd(int dtype, const NormShape& s, const void* x, const float* scale, const float* shift, void* y, float* mean,
                                  float* rstd, void* ws, hipStream_t st) {
@@ -829,6 +962,7 @@ hipError_t launch_group_norm_fwd(int dtype, const NormShape& s, const void* x, c
             }
             return over_images<T>(p, blocks_of(p, v), NT, [&](const NormParams& q, dim3 grid) {
                 hipLaunchKernelGGL((norm_sums_kernel<T, V.value>), grid, dim3(NT), 0, st, q);
+                join_groups<false>(q, st);
                 ProbeScope probe(st);
                 hipLaunchKernelGGL((norm_apply_kernel<T, V.value, A.value>), grid, dim3(NT), 0, st, q);
                 return hipGetLastError();
@@ -861,6 +995,7 @@ hipError_t launch_group_norm_bwd(int dtype, const NormShape& s, const void* x, c
             }
             return over_images<T>(p, blocks_of(p, v), NT, [&](const NormParams& q, dim3 grid) {
                 hipLaunchKernelGGL((norm_grad_sums_kernel<T, V.value, A.value>), grid, dim3(NT), 0, st, q);
+                join_groups<true>(q, st);
                 ProbeScope probe(st);
                 hipLaunchKernelGGL((norm_grad_apply_kernel<T, V.value, A.value>), grid, dim3(NT), 0, st, q);
                 return hipGetLastError();
