@@ -200,7 +200,8 @@ struct Shape {
     else if constexpr (AIN) { LIN_ASM(IN, OUT, SEQ, C, B); }      \
     else { LIN_ASM(OUT, OUT, SEQ, C, B); }
 
-// A 1024-byte load: LDS address, this lane's offset, the buffer. (M0 is the asm blocks' own here: nothing else in the kernel uses it.)
+// A 1024-byte load: LDS address, this lane's offset, the buffer. (M0 is the asm blocks' own here. The compiler reserves it and
+// warns of a clobber; that nothing else in these kernels uses it is tested on the code that it made.)
 struct Request { int to; unsigned off; u32x4 from; };
 __device__ __forceinline__ void request_now(const Request& q) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(q.to), "v"(q.off), "s"(q.from) : "memory");
