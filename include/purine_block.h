@@ -8,7 +8,7 @@
  * of N*H*W positions), so that its 1x1 layers are plain matrix products. The Python package's `blocks` module runs the
  * operators together as a training step.
  *
- * Activations, in fp32. GELU is z Phi(z), GELU_TANH 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))). act(-infinity) is the
+ * Activations, in fp32: of F32 tensors to a few units in the last place down to their tails, of BF16 ones to 1e-5 before the result is rounded. GELU is z Phi(z), GELU_TANH 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))). act(-infinity) is the
  * limit (0, but for NONE); NaNs stay NaNs. The slope of RELU at 0 is 0. */
 #ifndef PURINE_BLOCK_H
 #define PURINE_BLOCK_H

@@ -342,17 +342,17 @@ __global__ __launch_bounds__(NT) void norm_apply_kernel(const NormParams p) {
             float v[V];
             widen_v<T, V>(in[u], v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = act_of<ACT>((v[i] - mu[i]) * a[i] + b[i]);
+            for (int i = 0; i < V; ++i) v[i] = act_of<ACT, sizeof(T) == 4>((v[i] - mu[i]) * a[i] + b[i]);
             store_v<T, V>(y + (int64_t)(t + u * at.R) * p.C, v);
         }
     }
 }
 
 // x's place in its distribution and the gradient before the activation, of one element.
-template <int ACT>
+template <int ACT, bool FULL>
 __device__ __forceinline__ void grad_of(float x, float dy, float mu, float rstd, float scale, float shift, float& xhat, float& dz) {
     xhat = (x - mu) * rstd;
-    dz = dy * act_slope<ACT>(xhat * scale + shift);
+    dz = dy * act_slope<ACT, FULL>(xhat * scale + shift);
 }
 
 template <typename T, int V, int ACT>
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(NT, 4) void norm_grad_sums_kernel(const NormParams 
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     float xhat, dz;
-                    grad_of<ACT>(v[i], d[i], mu[i], rstd[i], sc[i], sh[i], xhat, dz);
+                    grad_of<ACT, sizeof(T) == 4>(v[i], d[i], mu[i], rstd[i], sc[i], sh[i], xhat, dz);
                     s[i] += dz;
                     q[i] += dz * xhat;
                 }
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(NT) void norm_grad_apply_kernel(const NormParams p)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 float xhat, dz;
-                grad_of<ACT>(v[i], d[i], mu[i], rstd[i], sc[i], sh[i], xhat, dz);
+                grad_of<ACT, sizeof(T) == 4>(v[i], d[i], mu[i], rstd[i], sc[i], sh[i], xhat, dz);
                 v[i] = dz * rs[i] - (xhat * c2[i] + c1[i]);
                 if (p.accumulate) v[i] += old[i];
             }
@@ -686,7 +686,7 @@ __global__ __launch_bounds__(THREADS) void norm_held_kernel(const NormParams p) 
         float v[V];
         widen_v<T, V>(in[u], v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = act_of<ACT>((v[i] - mu[i]) * a[i] + sh[i]);
+        for (int i = 0; i < V; ++i) v[i] = act_of<ACT, sizeof(T) == 4>((v[i] - mu[i]) * a[i] + sh[i]);
         store_v<T, V>(y + (int64_t)(r + u * R) * p.C, v);
     }
 }
@@ -729,7 +729,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_held_kernel(const NormParam
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 float xhat;
-                grad_of<ACT>(v[i], d[i], mu[i], rstd[i], sc[i], sh[i], xhat, dz[u][i]);
+                grad_of<ACT, sizeof(T) == 4>(v[i], d[i], mu[i], rstd[i], sc[i], sh[i], xhat, dz[u][i]);
                 s[i] += dz[u][i];
                 q[i] += dz[u][i] * xhat;
             }

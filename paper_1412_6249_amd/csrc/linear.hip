@@ -226,7 +226,7 @@ __global__ __launch_bounds__(ANT) void act_bwd_kernel(const ActParams p) {
                 if (row >= n) break;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    if (ACT != PURINE_ACT_NONE) v[u][e] *= act_slope<ACT>(z[u][e]);
+                    if (ACT != PURINE_ACT_NONE) v[u][e] *= act_slope<ACT, sizeof(T) == 4>(z[u][e]);
                     sum[e] += v[u][e];
                 }
                 if (p.g) lin::put_v(g + row * p.g_ld, v[u]);

@@ -28,8 +28,8 @@ template <typename E, typename O>
 __device__ __forceinline__ void finish(const Finish& f, int64_t i, int j, float z) {
     if (f.bias) z += widen<E>(((const E*)f.bias)[j]);
     if (f.pre) narrow(z, (E*)f.pre + i * f.pre_ld + j);
-    if (f.slope) z *= slope_any(f.act, widen<E>(((const E*)f.slope)[i * f.slope_ld + j]));
-    else z = act_any(f.act, z);
+    if (f.slope) z *= slope_any<sizeof(E) == 4>(f.act, widen<E>(((const E*)f.slope)[i * f.slope_ld + j]));
+    else z = act_any<sizeof(E) == 4>(f.act, z);
     if (f.res) z += widen<E>(((const E*)f.res)[i * f.res_ld + j]);
     O* o = (O*)f.out + i * f.out_ld + j;
     if (f.accumulate) z += widen<O>(*o);

@@ -455,13 +455,13 @@ __global__ __launch_bounds__(256, BI * BUFS > 256 ? 1 : BI * BUFS > 128 ? 2 : 4)
     auto combine = [&](float (&v)[8], const float (&t)[8], float (&pre)[8]) {
         if constexpr (EPI != PART && BIN) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { pre[e] = v[e] + bias[e]; v[e] = act_of<EPI>(pre[e]); }
+            for (int e = 0; e < 8; ++e) { pre[e] = v[e] + bias[e]; v[e] = act_of<EPI, false>(pre[e]); }
             if (reads)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += t[e];
         } else if constexpr (EPI != PART && EPI != PURINE_ACT_NONE) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= act_slope<EPI>(t[e]);
+            for (int e = 0; e < 8; ++e) v[e] *= act_slope<EPI, false>(t[e]);
         }
     };
     each<TI * 16 / ROWS>([&](auto H) {

@@ -126,13 +126,13 @@ __global__ __launch_bounds__(SWAVES * 64, 4) void linear_stream_kernel(const Str
                 if constexpr (BIN) {
                     const floatx4 b0 = *reinterpret_cast<const floatx4*>(bias + j), b1 = *reinterpret_cast<const floatx4*>(bias + j + 4);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { pre[e] = v[e] + (e < 4 ? b0[e & 3] : b1[e & 3]); v[e] = act_of<ACT>(pre[e]); }
+                    for (int e = 0; e < 8; ++e) { pre[e] = v[e] + (e < 4 ? b0[e & 3] : b1[e & 3]); v[e] = act_of<ACT, false>(pre[e]); }
                     if (reads)
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[e] += w[e];
                 } else if constexpr (ACT != PURINE_ACT_NONE) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] *= act_slope<ACT>(w[e]);
+                    for (int e = 0; e < 8; ++e) v[e] *= act_slope<ACT, false>(w[e]);
                 }
                 if (p.accumulate) {
                     lin::widen8(o[u], w);
