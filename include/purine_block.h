@@ -8,8 +8,9 @@
  * of N*H*W positions), so that its 1x1 layers are plain matrix products. The Python package's `blocks` module runs the
  * operators together as a training step.
  *
- * Activations, in fp32: of F32 tensors to a few units in the last place down to their tails, of BF16 ones to 1e-5 before the result is rounded. GELU is z Phi(z), GELU_TANH 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))). act(-infinity) is the
- * limit (0, but for NONE); NaNs stay NaNs. The slope of RELU at 0 is 0. */
+ * Activations, in fp32: of F32 tensors to a few units in the last place down to their tails, of BF16 ones to 1e-5 of themselves
+ * before the result is rounded. GELU is z Phi(z), GELU_TANH 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))). act(-infinity) is
+ * the limit (0, but for NONE); NaNs stay NaNs. The slope of RELU at 0 is 0. */
 #ifndef PURINE_BLOCK_H
 #define PURINE_BLOCK_H
 
@@ -47,8 +48,12 @@ int purine_group_norm_bwd(const purine_tensor* x, const purine_tensor* scale, co
 
 /* Matrix product with an epilogue: y = act(x w^T + b) + r, x [N, C], w [K, C], b [K], y [N, K], r [N, K], all F32 or all BF16.
  * b and r may be NULL. pre [N, K] (or NULL) receives x w^T + b, which the gradient needs. Matrices may set nstride, the
- * distance between rows (whole 16-byte packets): columns of wider buffers. y may be r itself. Sums are fp32; every result
- * is rounded once.
+ * distance between rows (whole 16-byte packets): columns of wider buffers. y may be r itself. Sums are fp32; every result of a
+ * call is rounded once.
+ * BF16: what the calls of a layer's gradient hand to each other is BF16 too, as the operands on the matrix cores are: pre, whose
+ * slope is taken at the rounded value, and the gradient before the activation (purine_act_bwd's g, or dx of the layer above).
+ * dx and dw of a layer with an activation so carry two roundings in a row and not one, 2.4e-3 of them in the 2-norm instead of
+ * the 1.7e-3 of fp32 values between; purine_act_bwd's db is summed before g is rounded. F32 tensors have none of this.
  * F32: three exact bf16 parts per operand and six products, as for convolutions (purine.h, "F32 arithmetic"); results that are infinite
  * or NaN are computed again as plain fp32 sums. Up to four rows of whole 16-byte packets: fp32 products.
  * pass for the workspace query: PURINE_CONV_FWD, _BWD_DATA, _BWD_WEIGHT. */
@@ -81,7 +86,8 @@ int purine_act_bwd(const purine_tensor* pre, const purine_tensor* dy, purine_ten
  * above 0 is never rounded to 0. Values that are not finite become NaN codes.
  * All tensors of a call share their types: w F32 or BF16 (rounded to nearest even), dw F32 or BF16, states F32 or F8 (m_scale and
  * v_scale are needed then, and ignored otherwise). copy: BF16 copy of the new w, or data = NULL. Each is dense, of w's
- * number of elements (the scales one per block, and aligned to 4 bytes only); tensors must not overlap. */
+ * number of elements (the scales one per block, and aligned to 4 bytes only); tensors must not overlap. The table of tensors is the
+ * caller's and only read: a program whose tensors stay where they are fills it once. */
 #define PURINE_ADAMW_BLOCK 256
 typedef struct {
     double lr, beta1, beta2, eps, weight_decay, grad_scale;

@@ -564,7 +564,10 @@ def _adamw_tensor_desc(t):
 
 
 def adamw_params(w, dw, m, v, m_scale=None, v_scale=None, copy=None):
-    """Lists of as many tensors each (m_scale, v_scale: with 8-bit states; copy: may be None or hold None)."""
+    """Lists of as many tensors each (m_scale, v_scale: with 8-bit states; copy: may be None or hold None).
+
+    For tensors that stay where they are, kept from step to step: it takes the host 5 us a tensor with fp32 states (64 us for 12, whose step takes 5.5),
+    which a program that allocates its gradients anew pays for every step."""
     n = len(w)
     lists = {"w": w, "dw": dw, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "copy": copy}
     for name, l in lists.items():

@@ -1,6 +1,6 @@
 // Activations of the block operators and their slopes, in fp32. FULL: for results of 32 bits, to a few units in their last place (the library's
 // exponential, a rounded quotient). Otherwise, for results that are rounded to bf16 (2e-3 of them): the hardware's power and reciprocal, whose error grows with the
-// exponent to some 1e-6 of the result. us, GELU and its slope on 64 x 12544 x 64 in fp32 within a normalization: FULL 364, otherwise 345.
+// exponent to some 1e-6 of the result. us, GELU and its slope on 64 x 12544 x 64 in fp32 within a normalization: FULL 364, short 344.
 #pragma once
 #include <hip/hip_runtime.h>
 

@@ -512,10 +512,12 @@ __device__ __forceinline__ float sum_over_block(float v, float* sums) {
 template <typename Member>
 __device__ __forceinline__ float3 join_members(unsigned count, float* sums, Member&& member) {
     float n, m, q, all = 0.0f, s = 0.0f;
+#pragma unroll 8
     for (unsigned i = threadIdx.x; i < count; i += NT) { member(i, n, m, q); all += n; s += n * m; }
     all = sum_over_block(all, sums);
     const float mean = sum_over_block(s, sums) / all;
     s = 0.0f;
+#pragma unroll 8
     for (unsigned i = threadIdx.x; i < count; i += NT) { member(i, n, m, q); s += q + n * ((m - mean) * (m - mean)); }
     return make_float3(all, mean, sum_over_block(s, sums));
 }
@@ -535,7 +537,7 @@ __global__ __launch_bounds__(NT) void norm_join_kernel(const NormParams p) {
     auto place = [=](unsigned i, unsigned& slice, unsigned& c) { slice = (first + i) / per; c = first + i - slice * per; };
     if constexpr (GRAD) {
         float a = 0.0f, b = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
         for (unsigned i = threadIdx.x; i < count; i += NT) {
             unsigned s, c;
             place(i, s, c);

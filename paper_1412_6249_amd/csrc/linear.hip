@@ -188,7 +188,8 @@ size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 size_t packed_bytes(int64_t rows, int64_t K, bool in, int planes) { return whole((size_t)(in ? rows * packed_ld(K) : K * packed_ld(rows)) * 2 * planes); }
 bool whole_packets(int64_t rows, int64_t K, bool in) { return (in ? K : rows) % 8 == 0; }
 
-// g = dy act'(pre), and the sums of its columns over a slice of the rows. Bound: HBM (us: 8192 x 8192 bf16 85, 403 MB at 4.7 TB/s; 100352 x 96 12.3,
+// g = dy act'(pre), and the sums of its columns over a slice of the rows. (g is rounded to the type that the products read, the sums are taken before: fp32 g
+// would be 4 bytes for 2 here and in two products, and three bf16 parts in them.) Bound: HBM (us: 8192 x 8192 bf16 85, 403 MB at 4.7 TB/s; 100352 x 96 12.3,
 // 58 MB at 4.7; 777 x 333 fp32 in single elements 4.4), then a launch of 4 - 5 for the slices' sums. A thread owns V neighbouring columns (16 bytes where
 // rows are whole packets) and walks down the slice, four rows at a time; the threads of a column join in LDS, the slices in a
 // second kernel, both in order.
