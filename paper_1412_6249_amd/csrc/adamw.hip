@@ -37,7 +37,7 @@ struct AdamwParams {
 };
 static_assert(sizeof(AdamwParams) <= 4096, "kernel arguments");
 
-// Two rounds of shift, exclusive or and an odd multiplier, the usual way to finish a hash; the multipliers are of that kind and no others were tried. Over 2^20
+// Two rounds of shift, exclusive or and an odd multiplier, as in published integer hashes (T. Mueller's has 0x45D9F3B twice); no other multipliers were tried. Over 2^20
 // inputs a bit of the input changes each bit of the output with a probability of 0.489 to 0.511, and the bytes for neighbouring elements correlate by less than 1e-3.
 __device__ __forceinline__ uint32_t mix(uint32_t h) {
     h = (h ^ (h >> 16)) * 0x45D9F3B3u;

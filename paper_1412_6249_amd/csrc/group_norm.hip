@@ -11,8 +11,8 @@
 // of a large common mean no digits are lost). For the gradient they are sum dz and sum dz xhat. Everything is joined in a fixed order.
 //
 // Bound: HBM, and with an activation the vector units nearly as much (about 30 instructions a gradient element). us, bf16: 128 x 784 x 192 in 32 groups, SiLU, held:
-// forward 20 (77 MB; 15 at the rate of a copy), gradient 34 (115 MB; 23); 64 x 12544 x 64 in 32 groups, GELU by tanh, sliced: sums 20 and result 38 (103 and 206 MB;
-// 20 and 40), gradient sums 43 and result 56 (206 and 308 MB; 40 and 60).
+// forward 21 (77 MB; 15 at the rate of a copy), gradient 34 (115 MB; 23); 64 x 12544 x 64 in 32 groups, GELU by tanh, sliced: sums 21 and result 38 (103 and 206 MB;
+// 20 and 40), gradient sums 45 and result 57 (206 and 308 MB; 40 and 60).
 //
 // Where an image's share of a few whole groups fits a workgroup's registers (norm_held_kernel, norm_grad_held_kernel), one workgroup reads it once and
 // writes the results: every tensor moves once. Otherwise (norm_sums / norm_apply) one kernel sums over slices of the positions and a second
@@ -786,8 +786,8 @@ int vector_of(int64_t C, int dtype) {
 // Channels of a workgroup that holds its share of an image in registers, its pieces per thread and its threads; no width where that does not apply.
 // Whole groups and whole pieces; as wide as fits up to a line of memory (128 bytes), unless that leaves fewer than 512 workgroups. Workgroups of
 // 256 threads where they hold 48 bytes of a row or more, else of 512: the more workgroups a compute unit has, the more their loads, sums and
-// stores overlap (us, bf16 forward: 256 x 196 x 256 in 128 bytes by 256 threads 15.6, by 512 19.7; 128 x 784 x 192 in 48 by 256 19.6, in 96 by 512 22.2; gradients gain 1
-// to 4%, those of fp32 lose as much).
+// stores overlap (us, bf16: 256 x 196 x 256 in 128 bytes by 256 threads forward 16.9 and gradient 26.7, by 512 22.0 and 26.8; 128 x 784 x 192 in 48 by 256 21.1 and
+// 34.5, in 96 by 512 22.6 and 36.6; gradients of fp32 lose as much).
 struct HeldPlan { int width, pieces, threads; };
 HeldPlan held_plan(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, int v, bool backward) {
     const int64_t per = C / G, bytes = dtype == PURINE_BF16 ? 2 : 4;
