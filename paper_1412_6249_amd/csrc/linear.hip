@@ -8,19 +8,20 @@ namespace purine {
 namespace {
 
 // Operands whose rows lie 2^24 elements apart or more, past the 32-bit offsets of the kernels on the matrix cores: 64 x 64 results per
-// workgroup, 16 per thread, fp32 products.
-struct FarParams { Source a, b; Finish f; int rows, cols, K, tiles_j; };
+// workgroup, 16 per thread, fp32 products. Where the rows themselves are that long, results are few (128 x 128 at most) and the reduction is split over some thousand
+// workgroups, whose sums the join adds (2 x 2^29 by 3 bf16 105 ms; one workgroup would need a thousand times that).
+struct FarParams { Source a, b; Finish f; int rows, cols, K, tiles_j, tiles; float* part; unsigned per; int part_ld; };    // part: of splits of `per`, or null
 constexpr int TS = 64, KS = 16;
 template <typename T, typename O>
 __global__ __launch_bounds__(256) void linear_far_kernel(const FarParams p) {
     __shared__ float as[KS][TS + 1], bs[KS][TS + 1];
-    const int i0 = (int)(blockIdx.x / p.tiles_j) * TS, j0 = (int)(blockIdx.x % p.tiles_j) * TS;
+    const int split = blockIdx.x / p.tiles, tile = (int)blockIdx.x - split * p.tiles, i0 = tile / p.tiles_j * TS, j0 = tile % p.tiles_j * TS;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const T* a = (const T*)p.a.p;
     const T* b = (const T*)p.b.p;
     float acc[4][4] = {};
-    const unsigned K = p.K;            // (k0 + k passes 2^31 where K is near it)
-    for (unsigned k0 = 0; k0 < K; k0 += KS) {
+    const unsigned first = split * p.per, K = min((unsigned)p.K, first + p.per);            // (k0 + k passes 2^31 where K is near it)
+    for (unsigned k0 = first; k0 < K; k0 += KS) {
         for (int e = threadIdx.x; e < KS * TS; e += 256) {
             const unsigned k = e / TS;
             const int i = e % TS;
@@ -36,7 +37,9 @@ __global__ __launch_bounds__(256) void linear_far_kernel(const FarParams p) {
     for (int u = 0; u < 4; ++u)
         for (int v = 0; v < 4; ++v) {
             const int i = i0 + ty * 4 + u, j = j0 + tx * 4 + v;
-            if (i < p.rows && j < p.cols) finish<T, O>(p.f, i, j, acc[u][v]);
+            if (i >= p.rows || j >= p.cols) continue;
+            if (p.part) p.part[((int64_t)split * p.rows + i) * p.part_ld + j] = acc[u][v];
+            else finish<T, O>(p.f, i, j, acc[u][v]);
         }
 }
 
@@ -68,9 +71,8 @@ __global__ __launch_bounds__(256) void linear_pack_kernel(const T* __restrict__ 
 // fp32 product's parts. Bound: memory (14173 x 4771 fp32, 541 MB: 147 us, rows that are no whole packets are stored element by element; with sums in such rows, one result a
 // thread, 252, and the product before it 305 for 169).
 struct JoinParams { const float* part; Finish f; Source a, b; int rows, cols, K, splits, lanes; };
-template <typename E, typename O>
+template <typename E, typename O, bool SPLIT3>
 __global__ __launch_bounds__(256) void linear_join_kernel(const JoinParams p) {
-    constexpr bool SPLIT3 = sizeof(E) == 4;
     __shared__ float sums[256][5];
     const int lanes = p.lanes, per = 256 / lanes, lane = threadIdx.x / per, mine = threadIdx.x % per;
     const unsigned chunks = (unsigned)(p.cols + 3) / 4, total = (unsigned)p.rows * chunks, t = blockIdx.x * (unsigned)per + mine;     // (below 2^31)
@@ -295,7 +297,17 @@ int act_rows(int64_t N, int64_t K, int V) {
 
 namespace {
 
-size_t piece_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_in, int dtype) {
+// Parts of the reduction in the kernel for far rows, where they are long themselves.
+constexpr int64_t FAR = (int64_t)1 << 24;
+int64_t far_splits(int64_t rows, int64_t cols, int64_t K) {
+    const int64_t tiles = ((rows + TS - 1) / TS) * ((cols + TS - 1) / TS);
+    return K >= FAR && tiles < 1024 ? 1024 / tiles : 1;
+}
+size_t far_ws_bytes(int64_t rows, int64_t cols, int64_t K) {
+    const int64_t splits = far_splits(rows, cols, K);
+    return splits > 1 ? (size_t)(splits * rows * part_ld(cols)) * 4 : 0;
+}
+size_t near_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_in, int dtype) {
     if (direct_form(rows, cols, K, a_in, b_in, dtype) != DIRECT_NONE) return 0;
     const int planes = dtype == PURINE_F32 ? 3 : 1;
     const GemmPlan g = plan_gemm(rows, cols, K, planes);
@@ -304,6 +316,10 @@ size_t piece_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_i
     if (planes == 3 || !whole_packets(cols, K, b_in)) n += packed_bytes(cols, K, b_in, planes);
     if (planes == 3 || g.splits > 1) n += (size_t)g.splits * rows * part_ld(cols) * 4;
     return n;
+}
+size_t piece_ws_bytes(int64_t rows, int64_t cols, int64_t K, bool a_in, bool b_in, int dtype) {
+    const size_t near = near_ws_bytes(rows, cols, K, a_in, b_in, dtype), far = a_in || b_in ? far_ws_bytes(rows, cols, K) : 0;
+    return near > far ? near : far;
 }
 
 // Rows and columns of a launch at most: a launch ends at 2^32 threads, and the single row's kernel has 64 for a column.
@@ -334,14 +350,14 @@ hipError_t by_parts(const LinearCall& c, int64_t rows, int64_t cols, F&& f) {
     return hipSuccess;
 }
 
-template <typename E, typename O>
+template <typename E, typename O, bool SPLIT3 = sizeof(E) == 4>
 hipError_t join(const JoinParams& q, hipStream_t st) {
     JoinParams p = q;
     const int64_t threads = (int64_t)p.rows * part_ld(p.cols) / 4;
     p.lanes = 1;
     while (p.lanes < 32 && p.lanes * 4 <= p.splits && threads * p.lanes < 256 * 512) p.lanes *= 2;
     const int64_t per = 256 / p.lanes, grid = (threads + per - 1) / per;
-    hipLaunchKernelGGL((linear_join_kernel<E, O>), dim3((unsigned)grid), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((linear_join_kernel<E, O, SPLIT3>), dim3((unsigned)grid), dim3(256), 0, st, p);
     return hipGetLastError();
 }
 
@@ -359,7 +375,7 @@ hipError_t launch_piece(const LinearCall& c, void* ws, hipStream_t st) {
     const Source a = source_of(c.a, c.a_ld, c.a_in), b = source_of(c.b, c.b_ld, c.b_in);
     (void)hipGetLastError();
     const DirectForm direct = direct_form(c.rows, c.cols, c.K, c.a_in, c.b_in, c.dtype);
-    const int64_t far = (int64_t)1 << 24, es = f32 ? 4 : 2;
+    const int64_t far = FAR, es = f32 ? 4 : 2;
     const int64_t span = ((c.a_in ? c.rows : c.K) * c.a_ld > (c.b_in ? c.cols : c.K) * c.b_ld ? (c.a_in ? c.rows : c.K) * c.a_ld : (c.b_in ? c.cols : c.K) * c.b_ld) * es;
     if (direct == DIRECT_STREAM) return launch_linear_stream(c, st);
     if (direct != DIRECT_NONE && span < 0x7fffffff) return launch_linear_direct(c, direct, st);
@@ -369,13 +385,21 @@ hipError_t launch_piece(const LinearCall& c, void* ws, hipStream_t st) {
         return by_parts(c, rows, cols, [&](const LinearCall& q) { return launch_linear_direct(q, direct, st); });
     }
     if (direct != DIRECT_NONE || c.a_ld >= far || c.b_ld >= far) {
-        FarParams p{a, b, f, (int)c.rows, (int)c.cols, (int)c.K, (int)((c.cols + TS - 1) / TS)};
-        const unsigned grid = (unsigned)((c.rows + TS - 1) / TS * p.tiles_j);
-        ProbeScope probe(st);
-        if (f32) hipLaunchKernelGGL((linear_far_kernel<float, float>), dim3(grid), dim3(256), 0, st, p);
-        else if (c.out_dtype == PURINE_F32) hipLaunchKernelGGL((linear_far_kernel<uint16_t, float>), dim3(grid), dim3(256), 0, st, p);
-        else hipLaunchKernelGGL((linear_far_kernel<uint16_t, uint16_t>), dim3(grid), dim3(256), 0, st, p);
-        return hipGetLastError();
+        const int64_t splits = c.a_in || c.b_in ? far_splits(c.rows, c.cols, c.K) : 1, per = (c.K + splits - 1) / splits;
+        FarParams p{a, b, f, (int)c.rows, (int)c.cols, (int)c.K, (int)((c.cols + TS - 1) / TS), 0, splits > 1 ? (float*)ws : nullptr, (unsigned)per, (int)part_ld(c.cols)};
+        p.tiles = (int)((c.rows + TS - 1) / TS) * p.tiles_j;
+        const unsigned grid = (unsigned)(p.tiles * splits);
+        {
+            ProbeScope probe(st);
+            if (f32) hipLaunchKernelGGL((linear_far_kernel<float, float>), dim3(grid), dim3(256), 0, st, p);
+            else if (c.out_dtype == PURINE_F32) hipLaunchKernelGGL((linear_far_kernel<uint16_t, float>), dim3(grid), dim3(256), 0, st, p);
+            else hipLaunchKernelGGL((linear_far_kernel<uint16_t, uint16_t>), dim3(grid), dim3(256), 0, st, p);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || splits == 1) return e;
+        const JoinParams q{p.part, f, a, b, p.rows, p.cols, p.K, (int)splits, 1};
+        if (f32) return join<float, float, false>(q, st);
+        return c.out_dtype == PURINE_F32 ? join<uint16_t, float>(q, st) : join<uint16_t, uint16_t>(q, st);
     }
     GemmPlan g = plan_gemm(c.rows, c.cols, c.K, planes);
     if (c.a_ld >= far / 4 || c.b_ld >= far / 4) {          // (a tile of 256 rows would span 2^31 bytes)
