@@ -422,24 +422,26 @@ __device__ __forceinline__ float2 group_averages(const NormParams& p, int lane, 
     return make_float2(sum(a) / count, sum(b) / count);
 }
 
-// dscale and dshift of 16 channels: 16 threads each share the images and slices, and join in LDS.
-__device__ __forceinline__ void param_sums(const NormParams& p, int first) {
+// dscale and dshift of 16 channels: 16 threads each share the images and slices, and join in LDS. They lie `stride` rows apart, `count` of them. Where there
+// are many, workgroups take PER of them each and leave their sums in the first (nobody else reads it), for a next launch.
+constexpr int PER = 1024;
+template <bool LAST>
+__global__ __launch_bounds__(NT) void norm_grad_params_kernel(const NormParams p, int from, int blocks, int64_t stride, int64_t count) {
     __shared__ float2 sums[16][17];
-    const int l = threadIdx.x & 15, r = threadIdx.x >> 4;
-    const unsigned c = (unsigned)first + l;
-    const int64_t rows = (int64_t)p.N * p.slices;
+    const int piece = LAST ? 0 : (int)(blockIdx.x / blocks), l = threadIdx.x & 15, r = threadIdx.x >> 4;
+    const unsigned c = (unsigned)from + (blockIdx.x - (unsigned)piece * blocks) * 16 + l;
+    const int64_t first = (int64_t)piece * PER, end = LAST || count - first < PER ? count : first + PER;
     float s = 0.0f, q = 0.0f;
     if (c < (unsigned)p.C)
 #pragma unroll 8
-        for (int64_t k = r; k < rows; k += 16) { const float2 o = p.part[k * p.C + c]; s += o.x; q += o.y; }
+        for (int64_t k = first + r; k < end; k += 16) { const float2 o = p.part[k * stride * p.C + c]; s += o.x; q += o.y; }
     sums[r][l] = make_float2(s, q);
     __syncthreads();
     if (r || c >= (unsigned)p.C) return;
     for (int k = 1; k < 16; ++k) { s += sums[k][l].x; q += sums[k][l].y; }
-    p.dshift[c] = s;
-    p.dscale[c] = q;
+    if (LAST) { p.dshift[c] = s; p.dscale[c] = q; }
+    else p.part[first * stride * p.C + c] = make_float2(s, q);
 }
-__global__ __launch_bounds__(NT) void norm_grad_params_kernel(const NormParams p, int from) { param_sums(p, from + (int)blockIdx.x * 16); }
 
 template <typename T, int V, int ACT>
 __global__ __launch_bounds__(NT) void norm_grad_apply_kernel(const NormParams p) {
@@ -938,6 +940,9 @@ hipError_t over_images(const NormParams& p, int64_t blocks, int threads, F&& lau
 
 }  // namespace
 
+// Rows of sums that one launch adds up for the parameters (us, bf16, both directions, N x 16 x 64 in 8 groups, in one launch / in two: 1500 images 34.0 / 33.4, 3000 59.2 / 55.8,
+// 12000 206 / 176; in one a thread goes through a chain of N / 128 batches of loads).
+constexpr int64_t MANY = 2048;
 // What the sliced kernels take, whichever a call gets (the held ones need a slice's at most).
 size_t group_norm_ws_bytes(int64_t N, int64_t S, int64_t C, int64_t G) { return sliced_plan(N, S, C, G).bytes; }
 
@@ -1005,10 +1010,15 @@ hipError_t launch_group_norm_bwd(int dtype, const NormShape& s, const void* x, c
         });
     });
     if (e != hipSuccess || !dscale) return e;
-    constexpr int64_t MOST = 16 << 23;             // channels of a launch: below 2^32 threads
+    constexpr int64_t MOST = 16 << 23;             // channels of a launch: below 2^32 threads (where there are more, images are few)
     for (int64_t from = 0; from < p.C; from += MOST) {
-        const int64_t channels = p.C - from < MOST ? p.C - from : MOST;
-        hipLaunchKernelGGL(norm_grad_params_kernel, dim3((unsigned)((channels + 15) / 16)), dim3(NT), 0, st, p, (int)from);
+        const int blocks = (int)(((p.C - from < MOST ? p.C - from : MOST) + 15) / 16);
+        int64_t stride = 1, count = (int64_t)p.N * p.slices;
+        for (; count > MANY; count = (count + PER - 1) / PER, stride *= PER) {
+            const int64_t pieces = (count + PER - 1) / PER;
+            hipLaunchKernelGGL((norm_grad_params_kernel<false>), dim3((unsigned)(blocks * pieces)), dim3(NT), 0, st, p, (int)from, blocks, stride, count);
+        }
+        hipLaunchKernelGGL((norm_grad_params_kernel<true>), dim3((unsigned)blocks), dim3(NT), 0, st, p, (int)from, blocks, stride, count);
     }
     return hipGetLastError();
 }

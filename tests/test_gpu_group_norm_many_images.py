@@ -51,3 +51,28 @@ def test_parameters_of_two_to_the_28_channels():
         xhat = (x[0, part].double().reshape(-1, 16) - mean[0, k // 16:part.stop // 16, None]) * rstd[0, k // 16:part.stop // 16, None]
         want = dy[0, part].double() * xhat.reshape(-1)
         assert bool(((ds[part].double() - want).abs() <= 8 * EPS * dy[0, part].double().abs() * (xhat.reshape(-1).abs() + 1)).all())
+
+
+@pytest.mark.parametrize("case", [((1 << 24) + 1001, 1, 8, 2), ((1 << 17) + 77, 3, 20, 5), (5000, 300, 12, 3), (2049, 1, 17, 1), (2048, 2, 40, 8), (300000, 1, 33, 3)],
+                         ids=lambda c: "x".join(map(str, c)))
+def test_parameters_of_many_images(case):
+    """Sums of terms of one sign over all images: 32 eps of the terms' magnitudes, however many there are."""
+    import paper_1412_6249_amd as pa
+    N, S, C, G = case
+    g = torch.Generator(device=DEV).manual_seed(2)
+    x = torch.randn(N, S, C, generator=g, device=DEV)
+    dy = torch.rand(N, S, C, generator=g, device=DEV) + 1.0
+    ws = torch.full((max(pa.purine_group_norm_workspace_bytes(b, (N, S, C), G) for b in (0, 1)),), 255, dtype=torch.uint8, device=DEV)
+    y = torch.empty_like(x)
+    mean, rstd = (torch.empty(N, G, device=DEV) for _ in range(2))
+    ds, db = (torch.full((C,), float("nan"), device=DEV) for _ in range(2))
+    pa.purine_group_norm_fwd(x, None, None, y, mean, rstd, G, 1e-2, pa.PURINE_ACT_NONE, ws=ws)
+    pa.purine_group_norm_bwd(x, None, None, mean, rstd, dy, y, ds, db, G, pa.PURINE_ACT_NONE, ws=ws)
+    want = torch.zeros(4, C, dtype=torch.float64, device=DEV)
+    for n in range(0, N, 1 << 20):
+        part = slice(n, n + (1 << 20))
+        xg, d = x[part].double().reshape(-1, S, G, C // G), dy[part].double().reshape(-1, C)
+        mu = xg.mean((1, 3), keepdim=True)
+        xhat = ((xg - mu) * ((xg - mu).pow(2).mean((1, 3), keepdim=True) + 1e-2).rsqrt()).reshape(-1, C)
+        want += torch.stack([(d * xhat).sum(0), d.sum(0), (2 * d * (xhat.abs() + 1)).sum(0), 2 * d.sum(0)])
+    assert bool(((ds.double() - want[0]).abs() <= 32 * EPS * want[2]).all()) and bool(((db.double() - want[1]).abs() <= 32 * EPS * want[3]).all())
