@@ -113,6 +113,7 @@ template <int THREADS>
 __device__ __forceinline__ void join_moments(float2* sums, int width, int R, int total) {
     constexpr int STEP = 16, AT_ONCE = 8;                           // (all sixteen at once would take the registers of a wavefront)
     const int columns = min(width, THREADS), lanes = THREADS / columns, c0 = threadIdx.x % columns, l = threadIdx.x / columns;
+    R = min(R, total);                                              // (no positions in rows past that)
     const int base = total / R;                                     // positions of a row: base, or one more in the first `more`
     const float each = (float)base, more = (float)(total - base * R), most = (float)R;
     __syncthreads();
